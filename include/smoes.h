@@ -16,9 +16,15 @@
  *   smoes_moe_forward      all of the above + grouped SwiGLU experts, shared
  *                          experts and the weighted combine
  *
+ * and, for a model that generates with the attention-accumulated score:
+ *
+ *   smoes_rotary_apply     rotary positions of queries and keys, and their gradient
+ *   smoes_kv_write, _read  paged cache of keys, values and scores (bf16 or e4m3)
+ *   smoes_attention_scores_decode  attention of one new token per sequence over it
+ *
  * Conventions shared by every entry point
  *   - Every array pointer is a DEVICE pointer owned by the caller; arrays are
- *     dense and row-major. The library allocates no device memory: scratch
+ *     dense and row-major (a token stride argument says where rows may lie apart). The library allocates no device memory: scratch
  *     comes from a caller-provided workspace whose size the matching
  *     *_workspace_size query returns (any alignment; the library aligns
  *     inside it). Workspace contents need not be initialised and are
@@ -646,6 +652,165 @@ int smoes_attention_scores(const void* q, const void* k, const void* v, int64_t 
 int smoes_attn_score_update(const void* x, const void* x_attn, int act_dtype, int64_t T, int d,
                             const float* m_heads, int n_heads, const float* m_in, float* m_out,
                             void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary positions of queries and keys.                                     */
+/* ------------------------------------------------------------------------ */
+
+#define SMOES_HEAD_DIM_MAX 512
+
+enum smoes_rotary_layout {
+    SMOES_ROTARY_HALF = 0,       /* pairs (i, i + rot_dim / 2) */
+    SMOES_ROTARY_INTERLEAVED = 1 /* pairs (2 i, 2 i + 1)       */
+};
+
+/* Frequencies of pair i < rot_dim / 2, with f_i = base^(-2 i / rot_dim) and s = factor. */
+enum smoes_rotary_scaling {
+    SMOES_ROTARY_UNSCALED = 0, /* f_i */
+    SMOES_ROTARY_LINEAR = 1,   /* f_i / s: positions interpolated */
+    SMOES_ROTARY_NTK = 2,      /* f_i with base s^(rot_dim / (rot_dim - 2)) times as large */
+    SMOES_ROTARY_BY_PARTS = 3  /* g f_i + (1 - g) f_i / s, g = clamp((n_i - beta_slow) / (beta_fast - beta_slow), 0, 1)
+                                  with n_i = original_len f_i / (2 pi) turns; amplitude 1 + 0.1 ln s */
+};
+
+typedef struct smoes_rotary {
+    int head_dim;         /* 2 .. SMOES_HEAD_DIM_MAX */
+    int rot_dim;          /* the first rot_dim values of a head are rotated: even, 2 .. head_dim */
+    int layout;           /* enum smoes_rotary_layout */
+    int scaling;          /* enum smoes_rotary_scaling */
+    double base;          /* > 0 (usually 10000) */
+    double factor;        /* s >= 1 (LINEAR, NTK, BY_PARTS) */
+    double original_len;  /* > 0 (BY_PARTS) */
+    double beta_fast;     /* > beta_slow (BY_PARTS; usually 32) */
+    double beta_slow;     /* >= 0 (BY_PARTS; usually 1) */
+} smoes_rotary;
+
+/*
+ * Host arithmetic: freqs[rot_dim / 2] (HOST doubles, radians per position) and
+ * the amplitude (HOST float) of desc. The caller keeps them and copies freqs
+ * to the device once. SMOES_ERR_ARG for a NULL pointer or a value out of
+ * range, SMOES_ERR_SHAPE for head_dim or rot_dim.
+ */
+int smoes_rotary_frequencies(const smoes_rotary* desc, double* freqs, float* amplitude);
+
+/*
+ * Pair (x, y) of token t and every head becomes, with the angle
+ * w = positions[t] freqs[i] and a = amplitude,
+ *   x' = a (x cos w - y sin w),  y' = a (x sin w + y cos w);
+ * values from rot_dim on are copied. backward = 1 applies the transpose
+ * (angle -w): q and k are then the gradients of the rotated tensors, the
+ * outputs those of the tensors before the rotation. Angles are float64, sines,
+ * cosines and products float32, results are rounded once to act_dtype.
+ * freqs      [rot_dim / 2] float64 (device).
+ * positions  [T] int32 (device, any sign), or NULL: token t is at position t.
+ * q, q_out   [T, n_heads, head_dim] act_dtype, the rows of a token dense, q_stride
+ *            and q_out_stride elements from token to token (a view into a fused
+ *            projection). k, k_out the same with n_kv_heads; n_kv_heads = 0: no keys.
+ *            An output may be its own input (same pointer and stride); any other
+ *            overlap is not allowed.
+ * desc's frequencies' fields are not read here, only head_dim, rot_dim and layout.
+ * SMOES_ERR_SHAPE for T >= 2^31 or a token stride below the row (T > 1).
+ * Asynchronous on `stream`; nothing is allocated.
+ */
+int smoes_rotary_apply(const smoes_rotary* desc, const double* freqs, float amplitude, const int32_t* positions,
+                       int64_t T, int act_dtype, int backward, const void* q, int64_t q_stride, int n_heads,
+                       void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, int n_kv_heads,
+                       void* k_out, int64_t k_out_stride, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged cache of keys, values and modality scores.                          */
+/* ------------------------------------------------------------------------ */
+
+enum smoes_kv_kind {
+    SMOES_KV_BF16 = 0, /* rows as bf16 */
+    SMOES_KV_E4M3 = 1  /* rows as e4m3 codes (OCP, 3 bits of mantissa, largest 448) of x / s, s = 2^e the smallest
+                          power of two, 2^-117 at least, with max |x| <= 448 s over the row's finite values (e = 0
+                          for a row of zeros), rounded to nearest even (but to 1.875 * 2^127 where that would
+                          pass the largest float32); NaN and infinities are kept as NaN. The scale byte is
+                          e + 127. What is read back, code * s, is a bf16 value. */
+};
+
+/*
+ * One layer's cache (device arrays of the caller). Page p holds page_size
+ * consecutive positions of one sequence:
+ *   k, v             [n_pages, n_kv_heads, page_size, head_dim] bf16 bits or e4m3 codes, 16-byte aligned
+ *   k_scale, v_scale [n_pages, n_kv_heads, page_size] uint8, 4-byte aligned (SMOES_KV_E4M3; else unused)
+ *   m                [n_pages, 2, page_size] float32, 16-byte aligned: vision and text scores of the
+ *                    layer's input, or NULL for a layer that carries none
+ * page_size: a power of two, 16 .. 4096; head_dim 64 or 128; 1 <= n_pages < 2^31.
+ * block_table [n_seq, max_pages] int32: page of positions j page_size ... of each
+ * sequence; max_pages * page_size < 2^31. An entry outside [0, n_pages) (e.g. -1)
+ * is a page that is not held. Sequences may share pages that neither writes.
+ * seq_lens [n_seq] int32: tokens of each sequence, those of the call included; one
+ * below 0 counts as 0.
+ */
+typedef struct smoes_kv_cache {
+    int64_t n_pages;
+    int page_size, n_kv_heads, head_dim, kind;
+    void* k;
+    void* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    float* m;
+} smoes_kv_cache;
+
+/*
+ * Append rows: token t of sequence b, with n_b = sample_offsets[b + 1] -
+ * sample_offsets[b] tokens in the call, goes to position
+ * seq_lens[b] - n_b + (t - sample_offsets[b]).
+ * sample_offsets [n_seq + 1] int32 (non-decreasing), or NULL: one token per
+ *            sequence, T = n_seq. Rows behind sample_offsets[n_seq] are not written.
+ * k, v       [T, n_kv_heads, head_dim] act_dtype (bf16 or float32), a token's rows
+ *            dense, k_stride and v_stride elements from token to token.
+ * m_in       [T, 2] float32 scores; required iff cache->m is not NULL.
+ * A token whose position is negative, at or behind max_pages * page_size, or on a
+ * page that is not held is not written. No two tokens of a call may have one place.
+ * Asynchronous on `stream`; nothing is allocated.
+ */
+int smoes_kv_write(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
+                   const int32_t* seq_lens, int n_seq, const int32_t* sample_offsets, int64_t T,
+                   const void* k, int64_t k_stride, const void* v, int64_t v_stride, int act_dtype,
+                   const float* m_in, void* stream);
+
+/*
+ * Read rows back: the same places as smoes_kv_write's, that is the last n_b
+ * tokens of every sequence (all of them with n_b = seq_lens[b]), dense, for
+ * smoes_attention_scores over a context that is in the cache.
+ * k, v       [T, n_kv_heads, head_dim] outputs of act_dtype, or NULL (not wanted).
+ * m          [T, 2] float32 output, or NULL.
+ * A token that has no place reads as zeros; rows behind sample_offsets[n_seq] are
+ * left as they were.
+ */
+int smoes_kv_read(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
+                  const int32_t* seq_lens, int n_seq, const int32_t* sample_offsets, int64_t T,
+                  void* k, void* v, int act_dtype, float* m, void* stream);
+
+/* Bytes of smoes_attention_scores_decode's workspace (0 for invalid sizes). Host arithmetic. */
+size_t smoes_attention_decode_workspace_size(const smoes_kv_cache* cache, int n_seq, int n_heads);
+
+/*
+ * smoes_attention_scores for one new token per sequence, over what the cache
+ * holds of positions 0 .. seq_lens[b] - 1 (the new token's own row is written
+ * first):
+ *   o[b][h]       = sum_j Attn_h(b, j) v[j][h_kv]     (bf16)
+ *   m_heads[b][h] = sum_j Attn_h(b, j) m[j]           (float32, 2 columns)
+ * with Attn_h(b, .) = softmax over the held positions j of scale * q[b][h] . k[j][h_kv]
+ * and h_kv = h / (n_heads / n_kv_heads). A sequence of which nothing is held (length 0, no
+ * page) gets zeros. Positions at or behind the length are not read, whatever their pages hold.
+ * q          [n_seq, n_heads, head_dim] bf16, q_stride elements from sequence to sequence.
+ * scale      logit scale; <= 0 selects 1 / sqrt(head_dim).
+ * o          [n_seq, n_heads, head_dim] bf16 output.
+ * m_heads    [n_seq, n_heads, 2] float32 output, as smoes_attn_score_update takes it;
+ *            required iff cache->m is not NULL.
+ * The cached rows enter as they are read back; products and sums are float32.
+ * The split of the work follows from all sequences' lengths: the same call gives
+ * the same bits. n_heads % n_kv_heads == 0, n_heads <= 65535. Asynchronous on `stream`;
+ * nothing is allocated; the workspace needs no initialisation.
+ */
+int smoes_attention_scores_decode(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
+                                  const int32_t* seq_lens, int n_seq, const void* q, int64_t q_stride, int n_heads,
+                                  float scale, void* o, float* m_heads, void* workspace, size_t workspace_bytes,
+                                  void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Timing helpers for stage_events (hipEvent_t handles behind void*).        */

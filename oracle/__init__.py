@@ -6,3 +6,4 @@ shares no code with the HIP path (which must never fall back to it).
 """
 from .smoes_oracle import *  # noqa: F401,F403
 from .smoes_oracle import GaussState, GmmState  # noqa: F401
+from . import serving_oracle as serving  # noqa: F401

@@ -1,6 +1,7 @@
 // C ABI of the SMoES layer: argument validation, workspace layout and the
 // launch sequence on the caller's stream. No call allocates device memory or
 // synchronises the host.
+#include <math.h>
 #include <stdio.h>
 
 #include "smoes.h"
@@ -46,6 +47,52 @@ int check_mi_shape(int64_t T, int E, int n_batch, int n_bins) {
     if (T < 0 || E < 1 || E > SMOES_E_MAX) return SMOES_ERR_SHAPE;
     if (n_bins < 1 || n_bins > SMOES_BINS_MAX || (E % n_bins) != 0) return SMOES_ERR_SHAPE;
     if (n_batch < 1) return SMOES_ERR_SHAPE;
+    return SMOES_OK;
+}
+
+static_assert(SMOES_HEAD_DIM_MAX == SMOES_HEAD_DIM_MAX_DEV, "the rotary kernels' LDS holds the largest head");
+
+int check_rotary(const smoes_rotary* r) {
+    if (r->head_dim < 2 || r->head_dim > SMOES_HEAD_DIM_MAX) return SMOES_ERR_SHAPE;
+    if (r->rot_dim < 2 || r->rot_dim > r->head_dim || (r->rot_dim % 2) != 0) return SMOES_ERR_SHAPE;
+    if (r->layout != SMOES_ROTARY_HALF && r->layout != SMOES_ROTARY_INTERLEAVED) return SMOES_ERR_ARG;
+    return SMOES_OK;
+}
+
+// The sizes of a cache and its block table; fills the sizes and arrays of `out`.
+int check_kv(const smoes_kv_cache* c, int64_t max_pages, int n_seq, KvCacheArgs* out) {
+    if (c == nullptr) return SMOES_ERR_ARG;
+    if (c->kind != SMOES_KV_BF16 && c->kind != SMOES_KV_E4M3) return SMOES_ERR_ARG;
+    if (c->n_pages < 1 || c->n_pages > INT32_MAX || n_seq < 0) return SMOES_ERR_SHAPE;
+    if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0) return SMOES_ERR_SHAPE;
+    if (c->n_kv_heads < 1 || c->n_kv_heads > 65535 || (c->head_dim != 64 && c->head_dim != 128)) return SMOES_ERR_SHAPE;
+    if (max_pages < 1 || max_pages > INT32_MAX / c->page_size) return SMOES_ERR_SHAPE;
+    out->n_pages = c->n_pages;
+    out->max_pages = max_pages;
+    out->page_shift = __builtin_ctz(static_cast<unsigned>(c->page_size));
+    out->n_kv_heads = c->n_kv_heads;
+    out->head_dim = c->head_dim;
+    out->e4m3 = c->kind == SMOES_KV_E4M3;
+    out->n_seq = n_seq;
+    out->k = c->k;
+    out->v = c->v;
+    out->k_scale = c->k_scale;
+    out->v_scale = c->v_scale;
+    out->m = c->m;
+    return SMOES_OK;
+}
+int check_kv_tokens(int64_t T, const smoes_kv_cache* c, int n_seq, const int32_t* sample_offsets) {
+    // token indexes are int32, and a workgroup takes at least one row of a token and head
+    if (T < 0 || T > INT32_MAX / 2 / c->n_kv_heads) return SMOES_ERR_SHAPE;
+    if (sample_offsets == nullptr && T != n_seq) return SMOES_ERR_SHAPE;
+    return SMOES_OK;
+}
+int check_kv_arrays(const smoes_kv_cache* c) {
+    auto off = [](const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; };
+    if (c->k == nullptr || c->v == nullptr || off(c->k, 16) || off(c->v, 16) || off(c->m, 16)) return SMOES_ERR_ARG;
+    if (c->kind == SMOES_KV_E4M3 &&
+        (c->k_scale == nullptr || c->v_scale == nullptr || off(c->k_scale, 4) || off(c->v_scale, 4)))
+        return SMOES_ERR_ARG;
     return SMOES_OK;
 }
 
@@ -245,6 +292,157 @@ int smoes_attn_score_update(const void* x, const void* x_attn, int act_dtype, in
         return SMOES_ERR_ARG;
     return hip_status(launch_attn_update(x, x_attn, act_dtype, T, d, m_heads, n_heads, m_in, m_out,
                                          as_stream(stream)));
+}
+
+// ------------------------------------------------------------------ rotary positions
+
+int smoes_rotary_frequencies(const smoes_rotary* r, double* freqs, float* amplitude) {
+    if (r == nullptr || freqs == nullptr || amplitude == nullptr) return SMOES_ERR_ARG;
+    const int st = check_rotary(r);
+    if (st != SMOES_OK) return st;
+    const double inf = HUGE_VAL;
+    if (r->scaling < SMOES_ROTARY_UNSCALED || r->scaling > SMOES_ROTARY_BY_PARTS) return SMOES_ERR_ARG;
+    if (!(r->base > 0.0 && r->base < inf)) return SMOES_ERR_ARG;
+    const bool scaled = r->scaling != SMOES_ROTARY_UNSCALED, parts = r->scaling == SMOES_ROTARY_BY_PARTS;
+    if (scaled && !(r->factor >= 1.0 && r->factor < inf)) return SMOES_ERR_ARG;
+    if (parts && !(r->original_len > 0.0 && r->original_len < inf && r->beta_slow >= 0.0 &&
+                   r->beta_fast > r->beta_slow && r->beta_fast < inf))
+        return SMOES_ERR_ARG;
+    const double dim = r->rot_dim;
+    double base = r->base;
+    // one pair turns by base^0 whatever the base
+    if (r->scaling == SMOES_ROTARY_NTK && r->rot_dim > 2) base *= pow(r->factor, dim / (dim - 2.0));
+    for (int i = 0; i < r->rot_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / dim);
+        if (r->scaling == SMOES_ROTARY_LINEAR) f /= r->factor;
+        if (parts) {
+            const double turns = r->original_len * f / 6.283185307179586;
+            const double g = fmin(1.0, fmax(0.0, (turns - r->beta_slow) / (r->beta_fast - r->beta_slow)));
+            f = g * f + (1.0 - g) * f / r->factor;
+        }
+        freqs[i] = f;
+    }
+    *amplitude = parts ? static_cast<float>(1.0 + 0.1 * log(r->factor)) : 1.0f;
+    return SMOES_OK;
+}
+
+int smoes_rotary_apply(const smoes_rotary* r, const double* freqs, float amplitude, const int32_t* positions,
+                       int64_t T, int act_dtype, int backward, const void* q, int64_t q_stride, int n_heads,
+                       void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, int n_kv_heads,
+                       void* k_out, int64_t k_out_stride, void* stream) {
+    if (r == nullptr || !dtype_ok(act_dtype)) return SMOES_ERR_ARG;
+    const int st = check_rotary(r);
+    if (st != SMOES_OK) return st;
+    if (amplitude != amplitude || (backward != 0 && backward != 1)) return SMOES_ERR_ARG;
+    if (T < 0 || T > INT32_MAX || n_heads < 1 || n_heads > 65535 || n_kv_heads < 0 || n_kv_heads > 65535)
+        return SMOES_ERR_SHAPE;
+    const int64_t q_row = static_cast<int64_t>(n_heads) * r->head_dim, k_row = static_cast<int64_t>(n_kv_heads) * r->head_dim;
+    if (T > 1 && (q_stride < q_row || q_out_stride < q_row)) return SMOES_ERR_SHAPE;
+    if (T > 1 && n_kv_heads > 0 && (k_stride < k_row || k_out_stride < k_row)) return SMOES_ERR_SHAPE;
+    if (T == 0) return SMOES_OK;
+    if (freqs == nullptr || q == nullptr || q_out == nullptr) return SMOES_ERR_ARG;
+    if (n_kv_heads > 0 && (k == nullptr || k_out == nullptr)) return SMOES_ERR_ARG;
+    if ((q == q_out && q_stride != q_out_stride && T > 1) ||
+        (n_kv_heads > 0 && k == k_out && k_stride != k_out_stride && T > 1))
+        return SMOES_ERR_ARG;
+    RotaryArgs a;
+    a.T = T;
+    a.head_dim = r->head_dim;
+    a.rot_dim = r->rot_dim;
+    a.interleaved = r->layout == SMOES_ROTARY_INTERLEAVED;
+    a.backward = backward;
+    a.n_heads = n_heads;
+    a.n_kv_heads = n_kv_heads;
+    a.amplitude = amplitude;
+    a.freqs = freqs;
+    a.positions = positions;
+    a.q = q;
+    a.k = k;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.q_out_stride = q_out_stride;
+    a.k_out_stride = k_out_stride;
+    return hip_status(launch_rotary(a, act_dtype, as_stream(stream)));
+}
+
+// ------------------------------------------------------------------ paged score cache
+
+int smoes_kv_write(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
+                   const int32_t* seq_lens, int n_seq, const int32_t* sample_offsets, int64_t T, const void* k,
+                   int64_t k_stride, const void* v, int64_t v_stride, int act_dtype, const float* m_in, void* stream) {
+    KvCacheArgs c;
+    if (!dtype_ok(act_dtype)) return SMOES_ERR_ARG;
+    int st = check_kv(cache, max_pages, n_seq, &c);
+    if (st == SMOES_OK) st = check_kv_tokens(T, cache, n_seq, sample_offsets);
+    if (st != SMOES_OK) return st;
+    const int64_t row = static_cast<int64_t>(cache->n_kv_heads) * cache->head_dim;
+    if (T > 1 && (k_stride < row || v_stride < row)) return SMOES_ERR_SHAPE;
+    if (T == 0 || n_seq == 0) return SMOES_OK;
+    if ((st = check_kv_arrays(cache)) != SMOES_OK) return st;
+    if (block_table == nullptr || seq_lens == nullptr || k == nullptr || v == nullptr) return SMOES_ERR_ARG;
+    if ((m_in != nullptr) != (cache->m != nullptr)) return SMOES_ERR_ARG;
+    c.T = T;
+    c.block_table = block_table;
+    c.seq_lens = seq_lens;
+    c.sample_offsets = sample_offsets;
+    return hip_status(launch_kv_write(c, k, k_stride, v, v_stride, act_dtype, m_in, as_stream(stream)));
+}
+
+int smoes_kv_read(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
+                  const int32_t* seq_lens, int n_seq, const int32_t* sample_offsets, int64_t T, void* k, void* v,
+                  int act_dtype, float* m, void* stream) {
+    KvCacheArgs c;
+    if (!dtype_ok(act_dtype)) return SMOES_ERR_ARG;
+    int st = check_kv(cache, max_pages, n_seq, &c);
+    if (st == SMOES_OK) st = check_kv_tokens(T, cache, n_seq, sample_offsets);
+    if (st != SMOES_OK) return st;
+    if (T == 0 || n_seq == 0) return SMOES_OK;
+    if ((st = check_kv_arrays(cache)) != SMOES_OK) return st;
+    if (block_table == nullptr || seq_lens == nullptr || (m != nullptr && cache->m == nullptr)) return SMOES_ERR_ARG;
+    if (k == nullptr && v == nullptr && m == nullptr) return SMOES_OK;
+    c.T = T;
+    c.block_table = block_table;
+    c.seq_lens = seq_lens;
+    c.sample_offsets = sample_offsets;
+    return hip_status(launch_kv_read(c, k, v, act_dtype, m, as_stream(stream)));
+}
+
+size_t smoes_attention_decode_workspace_size(const smoes_kv_cache* cache, int n_seq, int n_heads) {
+    KvCacheArgs c;
+    if (check_kv(cache, 1, n_seq, &c) != SMOES_OK || n_heads < 1 || n_heads > 65535 ||
+        (n_heads % cache->n_kv_heads) != 0)
+        return 0;
+    return decode_workspace_bytes(n_seq, n_heads, cache->n_kv_heads, cache->head_dim) + 2 * kAlign;
+}
+
+int smoes_attention_scores_decode(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
+                                  const int32_t* seq_lens, int n_seq, const void* q, int64_t q_stride, int n_heads,
+                                  float scale, void* o, float* m_heads, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+    KvCacheArgs c;
+    int st = check_kv(cache, max_pages, n_seq, &c);
+    if (st != SMOES_OK) return st;
+    if (n_heads < 1 || n_heads > 65535 || (n_heads % cache->n_kv_heads) != 0) return SMOES_ERR_SHAPE;
+    if (static_cast<int64_t>(n_seq) * n_heads > INT32_MAX) return SMOES_ERR_SHAPE;
+    if (n_seq > 1 && q_stride < static_cast<int64_t>(n_heads) * cache->head_dim) return SMOES_ERR_SHAPE;
+    if (scale != scale) return SMOES_ERR_ARG;
+    if (n_seq == 0) return SMOES_OK;
+    if ((st = check_kv_arrays(cache)) != SMOES_OK) return st;
+    if (block_table == nullptr || seq_lens == nullptr || q == nullptr || o == nullptr ||
+        (m_heads != nullptr) != (cache->m != nullptr))
+        return SMOES_ERR_ARG;
+    if (workspace == nullptr || workspace_bytes < smoes_attention_decode_workspace_size(cache, n_seq, n_heads))
+        return SMOES_ERR_WORKSPACE;
+    Carver w(workspace);
+    void* ws = w.take(decode_workspace_bytes(n_seq, n_heads, cache->n_kv_heads, cache->head_dim));
+    c.T = n_seq;
+    c.block_table = block_table;
+    c.seq_lens = seq_lens;
+    c.sample_offsets = nullptr;
+    const float sc = scale > 0.0f ? scale : 1.0f / sqrtf(static_cast<float>(cache->head_dim));
+    return hip_status(launch_decode(c, q, q_stride, n_heads, sc, o, m_heads, ws, as_stream(stream)));
 }
 
 size_t smoes_permute_workspace_size(int64_t T, int E, int k) { return permute_ws(T, E, k); }

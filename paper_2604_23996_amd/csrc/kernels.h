@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace smoes {
 
 // ---------------------------------------------------------------- router
@@ -207,5 +209,53 @@ hipError_t launch_attention(const void* q, const void* k, const void* v, int64_t
 hipError_t launch_attn_update(const void* x, const void* x_attn, int act_dtype, int64_t T, int d,
                               const float* m_heads, int H, const float* m_in, float* m_out, hipStream_t stream);
 hipError_t launch_attn_init(const uint8_t* modality_id, int64_t T, float* M, hipStream_t stream);
+
+// ---------------------------------------------------------------- rotary positions
+#define SMOES_HEAD_DIM_MAX_DEV 512
+struct RotaryArgs {
+    int64_t T;
+    int head_dim, rot_dim, interleaved, backward, n_heads, n_kv_heads;
+    float amplitude;
+    const double* freqs;       // [rot_dim / 2] radians per position
+    const int32_t* positions;  // [T] or NULL (the token index)
+    const void* q;
+    const void* k;
+    void* q_out;
+    void* k_out;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;  // elements from token to token
+};
+hipError_t launch_rotary(const RotaryArgs& a, int act_dtype, hipStream_t stream);
+
+// ---------------------------------------------------------------- paged score cache
+struct KvCacheArgs {
+    int64_t n_pages, max_pages, T;  // pages of the pool, of a block table row; tokens of this call
+    int page_shift;                 // log2 of the tokens of a page
+    int n_kv_heads, head_dim, e4m3, n_seq;
+    void* k;                        // [n_pages][n_kv_heads][page][head_dim], v too
+    void* v;
+    uint8_t* k_scale;               // [n_pages][n_kv_heads][page], v_scale too (e4m3)
+    uint8_t* v_scale;
+    float* m;                       // [n_pages][2][page] or NULL
+    const int32_t* block_table;     // [n_seq][max_pages]
+    const int32_t* seq_lens;        // [n_seq]
+    const int32_t* sample_offsets;  // [n_seq + 1] or NULL: token t is sequence t's only new one
+};
+// go(integral constants: head_dim, e4m3 cache, bf16 rows)
+template <class F>
+void kv_dispatch(const KvCacheArgs& c, bool bf16, F go) {
+    auto rows = [&](auto dh, auto e4m3) {
+        if (bf16) go(dh, e4m3, std::true_type{}); else go(dh, e4m3, std::false_type{});
+    };
+    auto kind = [&](auto dh) {
+        if (c.e4m3) rows(dh, std::true_type{}); else rows(dh, std::false_type{});
+    };
+    if (c.head_dim == 128) kind(std::integral_constant<int, 128>{}); else kind(std::integral_constant<int, 64>{});
+}
+hipError_t launch_kv_write(const KvCacheArgs& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                           int act_dtype, const float* m_in, hipStream_t stream);
+hipError_t launch_kv_read(const KvCacheArgs& c, void* k, void* v, int out_dtype, float* m, hipStream_t stream);
+size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim);
+hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, int H, float scale, void* o,
+                         float* m_heads, void* ws, hipStream_t stream);
 
 }  // namespace smoes

@@ -6,7 +6,8 @@ libsmoes.so. There is no fallback: if the library is missing this module
 raises when it is used.
 
 Names follow the C ABI in include/smoes.h: route, modality_score, mi_loss,
-permute, moe_forward (+ workspace helpers and the layer descriptor).
+permute, moe_forward (+ workspace helpers and the layer descriptor), rotary,
+kv_write, kv_read, attention_scores_decode.
 """
 from __future__ import annotations
 
@@ -68,6 +69,16 @@ class SmoesLayerGrads(ctypes.Structure):
 
 class SmoesStreams(ctypes.Structure):
     _fields_ = [("side", c_void * 2), ("events", c_void * 4)]
+
+
+class SmoesRotary(ctypes.Structure):
+    _fields_ = [("head_dim", c_int), ("rot_dim", c_int), ("layout", c_int), ("scaling", c_int)] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "original_len", "beta_fast", "beta_slow")]
+
+
+class SmoesKvCache(ctypes.Structure):
+    _fields_ = [("n_pages", c_i64), ("page_size", c_int), ("n_kv_heads", c_int), ("head_dim", c_int),
+                ("kind", c_int)] + [(n, c_void) for n in ("k", "v", "k_scale", "v_scale", "m")]
 
 
 def lib() -> ctypes.CDLL:
@@ -139,6 +150,24 @@ def lib() -> ctypes.CDLL:
         L.smoes_attn_score_update.restype = c_int
         L.smoes_attn_score_update.argtypes = [c_void, c_void, c_int, c_i64, c_int, c_void, c_int, c_void, c_void,
                                               c_void]
+        L.smoes_rotary_frequencies.restype = c_int
+        L.smoes_rotary_frequencies.argtypes = [ctypes.POINTER(SmoesRotary), c_void, c_void]
+        L.smoes_rotary_apply.restype = c_int
+        L.smoes_rotary_apply.argtypes = [ctypes.POINTER(SmoesRotary), c_void, c_float, c_void, c_i64, c_int, c_int,
+                                         c_void, c_i64, c_int, c_void, c_i64, c_void, c_i64, c_int, c_void, c_i64,
+                                         c_void]
+        L.smoes_kv_write.restype = c_int
+        L.smoes_kv_write.argtypes = [ctypes.POINTER(SmoesKvCache), c_void, c_i64, c_void, c_int, c_void, c_i64,
+                                     c_void, c_i64, c_void, c_i64, c_int, c_void, c_void]
+        L.smoes_kv_read.restype = c_int
+        L.smoes_kv_read.argtypes = [ctypes.POINTER(SmoesKvCache), c_void, c_i64, c_void, c_int, c_void, c_i64,
+                                    c_void, c_void, c_int, c_void, c_void]
+        L.smoes_attention_decode_workspace_size.restype = c_size
+        L.smoes_attention_decode_workspace_size.argtypes = [ctypes.POINTER(SmoesKvCache), c_int, c_int]
+        L.smoes_attention_scores_decode.restype = c_int
+        L.smoes_attention_scores_decode.argtypes = [ctypes.POINTER(SmoesKvCache), c_void, c_i64, c_void, c_int,
+                                                    c_void, c_i64, c_int, c_float, c_void, c_void, c_void, c_size,
+                                                    c_void]
         L.smoes_workspace_buffer.restype = c_int
         L.smoes_workspace_buffer.argtypes = [ctypes.POINTER(SmoesLayer), c_void, c_int, ctypes.POINTER(c_void),
                                              ctypes.POINTER(c_size)]
@@ -356,6 +385,256 @@ def attn_score_update(x: torch.Tensor, x_attn: torch.Tensor, m_heads: torch.Tens
     _check(lib().smoes_attn_score_update(_p(x), _p(x_attn), _dtype_code(x), T, d, _p(m_heads), H, _p(m_in),
                                          _p(out), _stream()), "smoes_attn_score_update")
     return out
+
+
+# ---------------------------------------------------------------- generating with the score: positions, cache, decode
+#
+# These take views: a tensor [tokens, heads, head_dim] may have any stride from token to token
+# (a slice of a fused projection). Tensors have to lie on one GPU; the work runs there, on that
+# GPU's current stream, whichever GPU is current.
+
+def _gpu_of(*tensors: Optional[torch.Tensor]) -> torch.device:
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("libsmoes takes tensors on a GPU")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("libsmoes takes tensors on one GPU")
+    return dev
+
+
+def _launch(dev: torch.device, where: str, fn, *args) -> None:
+    if dev.index == torch.cuda.current_device():
+        status = fn(*args, _stream())
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _stream())
+    if status != SMOES_OK:
+        raise SmoesError(status, where)
+
+
+def _heads(t: torch.Tensor, name: str, dtype=None, shape: Optional[Sequence[int]] = None) -> int:
+    """Checks a [tokens, heads, head_dim] tensor whose rows are dense inside a token; its token stride."""
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected {'[tokens, heads, head_dim]' if shape is None else tuple(shape)}, "
+                         f"got {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    n, h, d = t.shape
+    s0, s1, s2 = t.stride()
+    if n * h * d > 0 and ((d > 1 and s2 != 1) or (h > 1 and s1 != d) or (n > 1 and s0 < h * d)):
+        raise ValueError(f"{name}: the heads of a token have to be dense (strides {t.stride()})")
+    return s0 if n > 1 else h * d
+
+
+def _array(t: Optional[torch.Tensor], name: str, dtype, shape: Sequence[int]) -> None:
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a dense {tuple(shape)}, got {tuple(t.shape)}")
+
+
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
+
+
+@dataclass
+class RotarySpec:
+    """smoes_rotary: the first rot_dim values of a head are rotated (pairs i, i + rot_dim / 2 or
+    2 i, 2 i + 1), frequencies base^(-2 i / rot_dim) scaled for contexts longer than original_len."""
+    head_dim: int
+    rot_dim: int
+    layout: str = "half"
+    scaling: str = "none"
+    base: float = 10000.0
+    factor: float = 1.0
+    original_len: float = 4096
+    beta_fast: float = 32.0
+    beta_slow: float = 1.0
+
+    def c(self) -> SmoesRotary:
+        if self.layout not in ROTARY_LAYOUTS or self.scaling not in ROTARY_SCALINGS:
+            raise ValueError(f"layout in {sorted(ROTARY_LAYOUTS)}, scaling in {sorted(ROTARY_SCALINGS)}")
+        return SmoesRotary(self.head_dim, self.rot_dim, ROTARY_LAYOUTS[self.layout], ROTARY_SCALINGS[self.scaling],
+                           self.base, self.factor, self.original_len, self.beta_fast, self.beta_slow)
+
+
+def rotary_frequencies(spec: RotarySpec):
+    """smoes_rotary_frequencies: (float64 [rot_dim / 2] on the host, amplitude)."""
+    desc = spec.c()
+    freqs = torch.empty(max(spec.rot_dim // 2, 1), dtype=torch.float64)
+    amplitude = c_float()
+    _check(lib().smoes_rotary_frequencies(ctypes.byref(desc), _p(freqs), ctypes.byref(amplitude)),
+           "smoes_rotary_frequencies")
+    return freqs, float(amplitude.value)
+
+
+class RotaryPlan:
+    """A spec with its frequencies on the device: made once, used by every call of `rotary`."""
+
+    def __init__(self, spec: RotarySpec, device):
+        self.spec, self.desc = spec, spec.c()
+        freqs, self.amplitude = rotary_frequencies(spec)
+        self.freqs = freqs.to(device)
+
+
+def rotary(plan: RotaryPlan, q: torch.Tensor, k: Optional[torch.Tensor] = None,
+           positions: Optional[torch.Tensor] = None, backward: bool = False, q_out: Optional[torch.Tensor] = None,
+           k_out: Optional[torch.Tensor] = None):
+    """smoes_rotary_apply: q [T, H, head_dim] and k [T, Hkv, head_dim] at their int32 positions [T] (None:
+    0 .. T - 1); backward=True takes the gradients of the rotated tensors to those before the rotation.
+    Outputs are new dense tensors unless given (an input itself: in place). Returns (q_out, k_out or None)."""
+    dt, dh = _dtype_code(q), plan.spec.head_dim
+    q_stride = _heads(q, "q", None, (q.shape[0], q.shape[1], dh) if q.dim() == 3 else (-1, -1, dh))
+    T, H = q.shape[0], q.shape[1]
+    if q_out is None:
+        q_out = torch.empty((T, H, dh), dtype=q.dtype, device=q.device)
+    qo_stride = _heads(q_out, "q_out", q.dtype, q.shape)
+    Hkv = k_stride = ko_stride = 0
+    if k is not None:
+        Hkv = k.shape[1] if k.dim() == 3 else 0
+        k_stride = _heads(k, "k", q.dtype, (T, Hkv, dh))
+        if k_out is None:
+            k_out = torch.empty((T, Hkv, dh), dtype=q.dtype, device=q.device)
+        ko_stride = _heads(k_out, "k_out", q.dtype, k.shape)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    _array(positions, "positions", torch.int32, (T,))
+    dev = _gpu_of(plan.freqs, q, q_out, k, k_out, positions)
+    _launch(dev, "smoes_rotary_apply", lib().smoes_rotary_apply, plan.desc, plan.freqs.data_ptr(), plan.amplitude,
+            None if positions is None else positions.data_ptr(), T, dt, int(backward), q.data_ptr(), q_stride, H,
+            q_out.data_ptr(), qo_stride, None if k is None else k.data_ptr(), k_stride, Hkv,
+            None if k is None else k_out.data_ptr(), ko_stride)
+    return q_out, k_out
+
+
+KV_KINDS = {"bf16": 0, "e4m3": 1}
+
+
+class KVCache:
+    """One layer's paged cache (smoes_kv_cache): k, v [n_pages, n_kv_heads, page_size, head_dim] (bf16, or uint8
+    e4m3 codes with one uint8 scale exponent per token and head), m [n_pages, 2, page_size] float32 modality
+    scores (scores=False: none). Arrays are zeros unless given."""
+
+    def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, kind: str = "bf16",
+                 device="cuda", scores: bool = True, k: Optional[torch.Tensor] = None,
+                 v: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None, m: Optional[torch.Tensor] = None):
+        if kind not in KV_KINDS:
+            raise ValueError(f"kind in {sorted(KV_KINDS)}")
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.kind = \
+            n_pages, page_size, n_kv_heads, head_dim, kind
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+
+        def arr(t, name, dtype, shape):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=device)
+            _array(t, name, dtype, shape)
+            return t
+
+        dt = torch.bfloat16 if kind == "bf16" else torch.uint8
+        self.k, self.v = arr(k, "k", dt, shape), arr(v, "v", dt, shape)
+        self.k_scale = self.v_scale = self.m = None
+        if kind == "e4m3":
+            self.k_scale = arr(k_scale, "k_scale", torch.uint8, shape[:3])
+            self.v_scale = arr(v_scale, "v_scale", torch.uint8, shape[:3])
+        if scores or m is not None:
+            self.m = arr(m, "m", torch.float32, (n_pages, 2, page_size))
+        self.desc = SmoesKvCache(n_pages, page_size, n_kv_heads, head_dim, KV_KINDS[kind],
+                                 *(None if t is None else t.data_ptr()
+                                   for t in (self.k, self.v, self.k_scale, self.v_scale, self.m)))
+
+    def arrays(self):
+        return self.k, self.v, self.k_scale, self.v_scale, self.m
+
+
+def _kv_tables(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
+               sample_offsets: Optional[torch.Tensor]) -> int:
+    n_seq = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
+    _array(seq_lens, "seq_lens", torch.int32, (n_seq,))
+    _array(block_table, "block_table", torch.int32, (n_seq, block_table.shape[1] if block_table.dim() == 2 else -1))
+    _array(sample_offsets, "sample_offsets", torch.int32, (n_seq + 1,))
+    return n_seq
+
+
+def kv_write(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+             m_in: Optional[torch.Tensor] = None, sample_offsets: Optional[torch.Tensor] = None) -> None:
+    """smoes_kv_write: append rows k, v [T, Hkv, head_dim] (bf16 or float32) and scores m_in [T, 2] behind what
+    the sequences hold; seq_lens are the lengths with them. sample_offsets None: one token per sequence."""
+    n_seq = _kv_tables(cache, block_table, seq_lens, sample_offsets)
+    T = k.shape[0]
+    shape = (T, cache.n_kv_heads, cache.head_dim)
+    k_stride, v_stride = _heads(k, "k", None, shape), _heads(v, "v", k.dtype, shape)
+    _array(m_in, "m_in", torch.float32, (T, 2))
+    dev = _gpu_of(*cache.arrays(), block_table, seq_lens, k, v, m_in, sample_offsets)
+    _launch(dev, "smoes_kv_write", lib().smoes_kv_write, cache.desc, block_table.data_ptr(), block_table.shape[1],
+            seq_lens.data_ptr(), n_seq, None if sample_offsets is None else sample_offsets.data_ptr(), T,
+            k.data_ptr(), k_stride, v.data_ptr(), v_stride, _dtype_code(k),
+            None if m_in is None else m_in.data_ptr())
+
+
+def kv_read(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
+            sample_offsets: Optional[torch.Tensor] = None, T: Optional[int] = None, dtype=torch.bfloat16,
+            k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, m: Optional[torch.Tensor] = None):
+    """smoes_kv_read: the last tokens of every sequence as sample_offsets divides T rows among them (None: the
+    last one of each), as dense (k, v [T, Hkv, head_dim], m [T, 2] or None). Outputs are written into k, v, m
+    when given (rows behind the last sequence stay as they were), else new zeros of `dtype`."""
+    n_seq = _kv_tables(cache, block_table, seq_lens, sample_offsets)
+    if T is None:
+        T = k.shape[0] if k is not None else v.shape[0] if v is not None else n_seq if sample_offsets is None else None
+        if T is None:
+            raise ValueError("kv_read needs T, k or v when sample_offsets is given")
+    shape = (T, cache.n_kv_heads, cache.head_dim)
+    if k is not None or v is not None:
+        dtype = k.dtype if k is not None else v.dtype
+    k = torch.zeros(shape, dtype=dtype, device=cache.k.device) if k is None else k
+    v = torch.zeros(shape, dtype=dtype, device=cache.k.device) if v is None else v
+    _array(k, "k", dtype, shape)
+    _array(v, "v", dtype, shape)
+    if m is None and cache.m is not None:
+        m = torch.zeros((T, 2), dtype=torch.float32, device=cache.k.device)
+    _array(m, "m", torch.float32, (T, 2))
+    dev = _gpu_of(*cache.arrays(), block_table, seq_lens, k, v, m, sample_offsets)
+    _launch(dev, "smoes_kv_read", lib().smoes_kv_read, cache.desc, block_table.data_ptr(), block_table.shape[1],
+            seq_lens.data_ptr(), n_seq, None if sample_offsets is None else sample_offsets.data_ptr(), T,
+            k.data_ptr(), v.data_ptr(), _dtype_code(k), None if m is None else m.data_ptr())
+    return k, v, m
+
+
+def attention_decode_workspace_bytes(cache: KVCache, n_seq: int, n_heads: int) -> int:
+    return int(lib().smoes_attention_decode_workspace_size(cache.desc, n_seq, n_heads))
+
+
+def attention_scores_decode(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor, q: torch.Tensor,
+                            scale: float = 0.0, o: Optional[torch.Tensor] = None,
+                            m_heads: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """smoes_attention_scores_decode: attention of one new token per sequence, q [n_seq, H, head_dim] (bf16), over
+    the cache: (o [n_seq, H, head_dim] bf16, m_heads [n_seq, H, 2] float32 or None for a cache without scores).
+    Calls that may overlap in time (other streams, graphs replayed beside each other) need a workspace each."""
+    n_seq = _kv_tables(cache, block_table, seq_lens, None)
+    H = q.shape[1] if q.dim() == 3 else 0
+    q_stride = _heads(q, "q", torch.bfloat16, (n_seq, H, cache.head_dim))
+    if o is None:
+        o = torch.empty((n_seq, H, cache.head_dim), dtype=torch.bfloat16, device=q.device)
+    if m_heads is None and cache.m is not None:
+        m_heads = torch.empty((n_seq, H, 2), dtype=torch.float32, device=q.device)
+    _array(o, "o", torch.bfloat16, (n_seq, H, cache.head_dim))
+    _array(m_heads, "m_heads", torch.float32, (n_seq, H, 2))
+    if workspace is None:
+        workspace = _workspace(attention_decode_workspace_bytes(cache, n_seq, H), q.device)
+    _array(workspace, "workspace", torch.uint8, workspace.shape)
+    dev = _gpu_of(*cache.arrays(), block_table, seq_lens, q, o, m_heads, workspace)
+    _launch(dev, "smoes_attention_scores_decode", lib().smoes_attention_scores_decode, cache.desc,
+            block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(), n_seq, q.data_ptr(), q_stride, H,
+            scale, o.data_ptr(), None if m_heads is None else m_heads.data_ptr(), workspace.data_ptr(),
+            workspace.numel())
+    return o, m_heads
 
 
 def permute(topk_idx: torch.Tensor, E: int, x: Optional[torch.Tensor] = None):
