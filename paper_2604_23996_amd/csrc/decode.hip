@@ -1,6 +1,23 @@
 // Attention of one new token per sequence over the paged score cache (Sec. 3.2.1, Eq. 3 for a
 // token that is generated): o = sum_j p_j v_j and m = sum_j p_j M_j over the sequence's cached
-// tokens, p = softmax(scale q . k_j), with a running maximum and sum.
+// tokens, p = softmax(scale q . k_j), in one pass with a running maximum and sum.
+//
+// What bounds it is reading the cache once: 4 head_dim flops per key, value and query head, and at
+// most the 16 query heads of a group share a row. The work is cut evenly over a fixed number of
+// workgroups, whatever the sequences' lengths are: the tiles (DE_TILE keys of one sequence and
+// group) of all sequences stand in one row, and workgroup w takes tiles floor(w N / W) to
+// floor((w + 1) N / W). Lengths are only known on the device, so every workgroup counts the tiles
+// itself. A run of tiles of one (sequence, group) that a workgroup holds whole is finished by it;
+// of one that is shared, every workgroup leaves its maximum, sums and unscaled output in the
+// workspace, and decode_join_kernel puts them together.
+//
+// Layout, per wave and 16 keys: S^T = K Q^T with v_mfma_f32_16x16x32_bf16, A = K rows straight from
+// memory, B = the group's queries: lane l gets the logits of keys 4 (l / 16) + 0..3 and query l % 16.
+// O^T += V^T P^T with v_mfma_f32_16x16x4f32: product r's four keys are 4 k + r, so that its B operand
+// is register r of S^T after the exponential as it stands, and its A operand is what a lane loads
+// of row 4 (l / 16) + r, columns (l % 16) head_dim / 16 ...: a wave's loads are whole rows. Nothing moves
+// between lanes, and probabilities stay float32. A ninth product carries the scores: rows vision,
+// text and 1 (the softmax denominator).
 #include "common.h"
 #include "kernels.h"
 
@@ -10,102 +27,512 @@ namespace {
 
 constexpr int DE_THREADS = 256;
 constexpr int DE_WAVES = DE_THREADS / kWave;
+constexpr int DE_ROWS = 16;        // query heads of a group that are worked on together
+constexpr int DE_WORKERS = 768;    // three workgroups per CU
+constexpr float DE_LAZY = 8.f;     // the reference maximum moves when it is passed by this (log2)
 
-// One workgroup per (sequence, query head), a key per wave at a time.
-template <int DH, bool E4M3>
-__global__ void __launch_bounds__(DE_THREADS) decode_kernel(KvCacheArgs c, const uint16_t* __restrict__ q, int64_t q_stride,
-                                                            int H, float scale_log2, uint16_t* __restrict__ o,
-                                                            float* __restrict__ m_heads) {
-    constexpr int N = DH / kWave;
-    __shared__ float acc_s[DE_WAVES][DH], stat_s[DE_WAVES][5];
-    const int b = static_cast<int>(blockIdx.x) / H, hq = static_cast<int>(blockIdx.x) % H;
-    const int hk = hq / (H / c.n_kv_heads);
-    const int wave = threadIdx.x / kWave, lane = lane_id();
-    const int64_t cap = c.max_pages << c.page_shift;
-    const int len = static_cast<int>(min(static_cast<int64_t>(max(c.seq_lens[b], 0)), cap));
-    float qv[N], acc[N] = {};
+// Layout of the workspace: 2 partial results per worker, then the plan that the join reads.
+struct DecodePlan {
+    int64_t total;  // tiles of all sequences and groups
+};
+__host__ __device__ constexpr int partial_floats(int rows, int dh) { return rows * (dh + 4); }
+
+struct DecodeArgs {
+    int64_t n_pages, max_pages, q_stride;
+    int page_shift, n_kv_heads, n_seq, H, group, rgroups, rows;  // rows: query heads per tile of 16
+    float scale_log2;
+    const uint8_t* k;
+    const uint8_t* v;
+    const uint8_t* k_scale;
+    const uint8_t* v_scale;
+    const float* m;
+    uint16_t* o;
+    float* m_heads;
+};
+
+__device__ __forceinline__ int seq_tiles(int len, int64_t cap, int tile) {
+    const int64_t n = min(static_cast<int64_t>(max(len, 0)), cap);
+    return static_cast<int>((n + tile - 1) / tile);
+}
+
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+
+// NS: 16-key pieces of a wave per tile.
+template <int DH, bool E4M3, int NS>
+struct DecodeTile {
+    static constexpr int ES = E4M3 ? 1 : 2;
+    static constexpr int KL = DH * ES / 64;        // 16-byte loads of a key row piece per lane
+    static constexpr int VB = DH * ES / 16;        // bytes of a value row per lane
+    static constexpr int VN = DH / 16;             // values of them
+    static constexpr int TILE = DE_WAVES * 16 * NS;
+    i32x4_t k[NS][KL];
+    int v[NS][4][VB / 4];
+    i32x4_t m[NS];
+    int ks[NS], vs[NS];
+    int nk[NS], nv[NS];  // rows that are held, of the pieces in k and in v
+};
+
+template <int VB>
+__device__ __forceinline__ void load_v(__amdgpu_buffer_rsrc_t r, int off, int (&x)[VB / 4]) {
+    if constexpr (VB == 16) {
+        const auto t = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) qv[i] = bf16_to_f32(q[b * q_stride + static_cast<int64_t>(hq) * DH + lane * N + i]);
-    float mx = -INFINITY, l = 0.f, a0 = 0.f, a1 = 0.f, seen = 0.f;
-    for (int j = wave; j < len; j += DE_WAVES) {
-        const int page = c.block_table[b * c.max_pages + (j >> c.page_shift)];
-        if (page < 0 || page >= c.n_pages) continue;
-        const int s = j & ((1 << c.page_shift) - 1);
-        const int64_t slot = ((static_cast<int64_t>(page) * c.n_kv_heads + hk) << c.page_shift) + s;
-        float kx[N], vx[N];
+        for (int i = 0; i < 4; ++i) x[i] = static_cast<int>(t[i]);
+    } else if constexpr (VB == 8) {
+        const auto t = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+        x[0] = static_cast<int>(t[0]);
+        x[1] = static_cast<int>(t[1]);
+    } else {
+        x[0] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+    }
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, kBufferFlags);
+}
+
+template <int DH, bool E4M3, int NS>
+__global__ void __launch_bounds__(DE_THREADS)
+decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __restrict__ block_table,
+              const int32_t* __restrict__ seq_lens, float* __restrict__ part, int64_t* __restrict__ plan) {
+    using T = DecodeTile<DH, E4M3, NS>;
+    constexpr int NQ = DH / 32;  // 32-wide slices of the logits' contraction
+    constexpr int PITCH = DH + 4;
+    __shared__ __attribute__((aligned(16))) float acc_s[DE_WAVES][DE_ROWS][PITCH];
+    __shared__ float max_s[DE_WAVES][DE_ROWS];
+    __shared__ int64_t scan_s[DE_WAVES];
+    __shared__ int64_t found_s[2];
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave), lane = lane_id();
+    const int l16 = lane & 15, g4 = lane >> 4;
+    const int64_t cap = a.max_pages << a.page_shift;
+    const int HR = a.n_kv_heads * a.rgroups;
+    const int w = static_cast<int>(blockIdx.x), W = static_cast<int>(gridDim.x);
+
+    // ---- the plan: all tiles, this workgroup's range, and where it starts
+    // sum over 256 sequences at a time of their tiles: inclusive prefix of this thread's, and the whole
+    auto scan = [&](int n, int64_t& incl) {
+        int64_t x = n;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int64_t at = slot * DH + lane * N + i;
-            if constexpr (E4M3) {
-                kx[i] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(c.k)[at], 0) *
-                        __uint_as_float(static_cast<uint32_t>(c.k_scale[slot]) << 23);
-                vx[i] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(c.v)[at], 0) *
-                        __uint_as_float(static_cast<uint32_t>(c.v_scale[slot]) << 23);
-            } else {
-                kx[i] = bf16_to_f32(static_cast<const uint16_t*>(c.k)[at]);
-                vx[i] = bf16_to_f32(static_cast<const uint16_t*>(c.v)[at]);
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int64_t y = __shfl_up(x, d, kWave);
+            if (lane >= d) x += y;
+        }
+        __syncthreads();
+        if (lane == kWave - 1) scan_s[wave] = x;
+        __syncthreads();
+        int64_t before = 0, all = 0;
+#pragma unroll
+        for (int i = 0; i < DE_WAVES; ++i) {
+            before += i < wave ? scan_s[i] : 0;
+            all += scan_s[i];
+        }
+        incl = before + x;
+        return all;
+    };
+    int64_t total = 0, incl0 = 0;
+    int n0 = 0;
+    for (int b0 = 0; b0 < a.n_seq; b0 += DE_THREADS) {
+        const int b = b0 + static_cast<int>(threadIdx.x);
+        n0 = b < a.n_seq ? seq_tiles(seq_lens[b], cap, T::TILE) : 0;
+        const int64_t before = total;
+        total += scan(n0, incl0);
+        // the join wants to know where every sequence's tiles start
+        if (w == 0 && b < a.n_seq) plan[1 + b] = (before + incl0 - n0) * HR;
+    }
+    total *= HR;
+    if (w == 0 && threadIdx.x == 0) plan[0] = total;
+    int64_t g = total * w / W;  // total < 2^31 tiles of 16 keys at least x 65535 heads: the product fits
+    const int64_t g_end = total * (w + 1) / W;
+    if (g == g_end) return;
+    {
+        int64_t before = 0;
+        for (int b0 = 0; b0 < a.n_seq; b0 += DE_THREADS) {
+            if (a.n_seq > DE_THREADS) {
+                const int b = b0 + static_cast<int>(threadIdx.x);
+                n0 = b < a.n_seq ? seq_tiles(seq_lens[b], cap, T::TILE) : 0;
+                const int64_t all = scan(n0, incl0);
+                incl0 += before;
+                before += all;
+            }
+            if (n0 > 0 && (incl0 - n0) * HR <= g && g < incl0 * HR) {
+                found_s[0] = b0 + static_cast<int>(threadIdx.x);
+                found_s[1] = g - (incl0 - n0) * HR;
             }
         }
-        float dot = 0.f;
+        __syncthreads();
+    }
+    int b = __builtin_amdgcn_readfirstlane(static_cast<int>(found_s[0]));
+    int len = static_cast<int>(min(static_cast<int64_t>(max(seq_lens[b], 0)), cap));
+    int nb = (len + T::TILE - 1) / T::TILE;
+    const int64_t in_seq = found_s[1];
+    int hr = __builtin_amdgcn_readfirstlane(static_cast<int>(in_seq / nb));
+    int i0 = __builtin_amdgcn_readfirstlane(static_cast<int>(in_seq % nb));
+    bool first = true;
+
+    // ---- runs of tiles
+    while (true) {
+        const int i1 = static_cast<int>(min(static_cast<int64_t>(nb), i0 + (g_end - g)));
+        const int hk = hr / a.rgroups, row0 = (hr % a.rgroups) * DE_ROWS;
+        const int rows = min(DE_ROWS, a.group - row0);
+        const int32_t* table = block_table + b * a.max_pages;
+
+        // queries of the group as B fragments: slice c of lane l holds query l % 16, the dims of the
+        // key fragment it meets
+        bf16x8_t qf[NQ];
+        {
+            typedef int i32x4_u __attribute__((ext_vector_type(4), aligned(2)));
+            const uint16_t* qr = q + b * a.q_stride + static_cast<int64_t>(hk * a.group + row0 + min(l16, rows - 1)) * DH;
 #pragma unroll
-        for (int i = 0; i < N; ++i) dot = fmaf(qv[i], kx[i], dot);
-        // as long as every logit is minus infinity, exponents are taken from 0: their sum stays 0
-        const float x = wave_sum_u(dot) * scale_log2, mn = fmaxf(mx, x), from = mn == -INFINITY ? 0.f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(mx - from), p = __builtin_amdgcn_exp2f(x - from);
-        mx = mn;
-        seen = 1.f;
-        l = l * alpha + p;
-        if (c.m != nullptr) {
-            const float* mp = c.m + ((static_cast<int64_t>(page) * 2) << c.page_shift) + s;
-            a0 = a0 * alpha + p * mp[0];
-            a1 = a1 * alpha + p * mp[1 << c.page_shift];
+            for (int c = 0; c < NQ; ++c) {
+                const int d = E4M3 ? 64 * (c >> 1) + 16 * g4 + 8 * (c & 1) : 32 * c + 8 * g4;
+                qf[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const i32x4_u*>(qr + d));
+            }
         }
+
+        T t;
+        int page[NS], held[NS];
+        // pages of tile i's pieces of this wave, and how many of their rows are held (0: past the end, no page)
+        auto pages = [&](int i) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = acc[i] * alpha + p * vx[i];
-    }
+            for (int s = 0; s < NS; ++s) {
+                const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
+                const bool in = i < i1 && pos < len;
+                const int p = in ? table[pos >> a.page_shift] : -1;
+                const bool ok = p >= 0 && p < a.n_pages;
+                page[s] = ok ? p : 0;
+                held[s] = ok ? min(16, len - pos) : 0;
+            }
+        };
+        // first row of piece s of tile i in the pool's rows of one head
+        auto row_of = [&](int i, int s) {
+            const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
+            return ((static_cast<int64_t>(page[s]) * a.n_kv_heads + hk) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+        };
+        // rows that are not held are outside their buffer: they read as zeros and cost nothing
+        auto load_k = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc_s[wave][lane * N + i] = acc[i];
-    if (lane == 0) {
-        stat_s[wave][0] = mx;
-        stat_s[wave][1] = l;
-        stat_s[wave][2] = a0;
-        stat_s[wave][3] = a1;
-        stat_s[wave][4] = seen;
+            for (int s = 0; s < NS; ++s) {
+                const int64_t row = row_of(i, s);
+                const auto r = rsrc(a.k + row * (DH * T::ES), held[s] * DH * T::ES);
+#pragma unroll
+                for (int c = 0; c < T::KL; ++c) {
+                    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, l16 * DH * T::ES + g4 * 16 + c * 64, 0, 0);
+                    t.k[s][c] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
+                }
+                if constexpr (E4M3)
+                    t.ks[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale + row, (held[s] + 3) & ~3), g4 * 4, 0, 0));
+                t.nk[s] = held[s];
+            }
+        };
+        auto load_v_m = [&](int i) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int64_t row = row_of(i, s);
+                const auto r = rsrc(a.v + row * (DH * T::ES), held[s] * DH * T::ES);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) load_v<T::VB>(r, (g4 * 4 + e) * DH * T::ES + l16 * T::VB, t.v[s][e]);
+                if constexpr (E4M3)
+                    t.vs[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale + row, (held[s] + 3) & ~3), g4 * 4, 0, 0));
+                // vision scores for lanes l % 16 = 0, text for 1; the others read nothing
+                const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
+                const float* mp = a.m + ((static_cast<int64_t>(page[s]) * 2) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+                const auto rm = rsrc(mp, a.m != nullptr && held[s] > 0 ? (4 << a.page_shift) + 64 : 0);
+                const auto x = __builtin_amdgcn_raw_buffer_load_b128(rm, l16 < 2 ? (l16 << (a.page_shift + 2)) + g4 * 16 : kOutOfRange, 0, 0);
+                t.m[s] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
+                t.nv[s] = held[s];
+            }
+        };
+
+        f32x4_t acc[T::VN + 1];
+#pragma unroll
+        for (int n = 0; n <= T::VN; ++n) acc[n] = f32x4_t{};
+        float m_run = -INFINITY;
+        bool seen = false;
+
+        pages(i0);
+        load_k(i0);
+        load_v_m(i0);
+        for (int i = i0; i < i1; ++i) {
+            pages(i + 1);
+            // ---- logits, in units of log2
+            f32x4_t s[NS];
+            float mx = -INFINITY;
+#pragma unroll
+            for (int p = 0; p < NS; ++p) {
+                s[p] = f32x4_t{};
+#pragma unroll
+                for (int c = 0; c < NQ; ++c) {
+                    bf16x8_t kf;
+                    if constexpr (E4M3) {
+                        // e4m3 values are bf16 values; the row's scale goes to the logit
+                        union { bf16x8_t v; bf16x2_t h[4]; } u;
+                        const int x0 = t.k[p][c >> 1][2 * (c & 1)], x1 = t.k[p][c >> 1][2 * (c & 1) + 1];
+                        u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, 1.f, false);
+                        u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, 1.f, true);
+                        u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, 1.f, false);
+                        u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, 1.f, true);
+                        kf = u.v;
+                    } else {
+                        kf = __builtin_bit_cast(bf16x8_t, t.k[p][c]);
+                    }
+                    s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c], s[p], 0, 0, 0);
+                }
+                const int nk = t.nk[p];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = s[p][e] * a.scale_log2;
+                    if constexpr (E4M3) x *= __uint_as_float((static_cast<uint32_t>(t.ks[p]) >> (8 * e) & 0xffu) << 23);
+                    x = g4 * 4 + e < nk ? x : -INFINITY;
+                    s[p][e] = x;
+                    mx = fmaxf(mx, x);
+                }
+                seen |= nk > 0;
+            }
+            load_k(i + 1);
+            // ---- running maximum, moved lazily
+            mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            const bool grow = mx > m_run + DE_LAZY;
+            if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+                const float m_new = grow ? mx : m_run;
+                const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
+                m_run = m_new;
+#pragma unroll
+                for (int n = 0; n <= T::VN; ++n) acc[n] *= alpha;
+            }
+            // as long as every logit is minus infinity, exponents are taken from 0: their sum stays 0
+            const float from = m_run == -INFINITY ? 0.f : m_run;
+            // ---- probabilities, values, scores
+#pragma unroll
+            for (int p = 0; p < NS; ++p) {
+                const int nv = t.nv[p];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = g4 * 4 + e < nv;
+                    const float pr = __builtin_amdgcn_exp2f(s[p][e] - from);
+                    float pv = pr;
+                    if constexpr (E4M3) pv = in ? pr * __uint_as_float((static_cast<uint32_t>(t.vs[p]) >> (8 * e) & 0xffu) << 23) : 0.f;
+                    const float mc = l16 == 2 ? 1.f : in ? __int_as_float(t.m[p][e]) : 0.f;
+#pragma unroll
+                    for (int n = 0; n < T::VN; n += 2) {
+                        float v0, v1;
+                        if constexpr (E4M3) {
+                            const auto y = (n & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8(t.v[p][e][n / 4], true)
+                                                   : __builtin_amdgcn_cvt_pk_f32_fp8(t.v[p][e][n / 4], false);
+                            v0 = y[0];
+                            v1 = y[1];
+                        } else {
+                            const uint32_t y = static_cast<uint32_t>(t.v[p][e][n / 2]);
+                            v0 = __uint_as_float(y << 16);
+                            v1 = __uint_as_float(y & 0xffff0000u);
+                        }
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v0, pv, acc[n], 0, 0, 0);
+                        acc[n + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v1, pv, acc[n + 1], 0, 0, 0);
+                    }
+                    acc[T::VN] = __builtin_amdgcn_mfma_f32_16x16x4f32(mc, pr, acc[T::VN], 0, 0, 0);
+                }
+            }
+            load_v_m(i + 1);
+        }
+
+        // ---- the four waves' results of this run: common maximum, then sums through LDS
+        __syncthreads();  // the last run's are read
+        if (g4 == 0) max_s[wave][l16] = m_run;
+        __syncthreads();
+        float mt = max_s[0][l16];
+#pragma unroll
+        for (int i = 1; i < DE_WAVES; ++i) mt = fmaxf(mt, max_s[i][l16]);
+        const float wt = __builtin_amdgcn_exp2f(m_run - (mt == -INFINITY ? 0.f : mt));
+        // element e of acc[n]: dim (4 (l / 16) + e) VN + n of query l % 16
+        float* row = acc_s[wave][l16];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int n = 0; n < T::VN; n += 4)
+                *reinterpret_cast<f32x4_t*>(row + (4 * g4 + e) * T::VN + n) =
+                    f32x4_t{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]} * wt;
+        if (g4 == 0)  // vision, text, sum (-1: no key seen), maximum
+            *reinterpret_cast<f32x4_t*>(row + DH) =
+                f32x4_t{acc[T::VN][0] * wt, acc[T::VN][1] * wt, seen ? acc[T::VN][2] * wt : -1.f, mt};
+        __syncthreads();
+        const bool whole = i0 == 0 && i1 == nb;
+        float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH);
+        for (int x = threadIdx.x; x < rows * (DH / 4); x += DE_THREADS) {
+            const int r = x / (DH / 4), d = x % (DH / 4) * 4;
+            f32x4_t sum = f32x4_t{};
+            float l = 0.f;
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < DE_WAVES; ++i) {
+                sum += *reinterpret_cast<const f32x4_t*>(&acc_s[i][r][d]);
+                const float li = acc_s[i][r][DH + 2];
+                any |= li != -1.f;
+                l += li != -1.f ? li : 0.f;
+            }
+            const int64_t head = static_cast<int64_t>(b) * a.H + hk * a.group + row0 + r;
+            f32x4_t st{};
+            if (d == 0) {
+#pragma unroll
+                for (int i = 0; i < DE_WAVES; ++i) {
+                    st[0] += acc_s[i][r][DH];
+                    st[1] += acc_s[i][r][DH + 1];
+                }
+                st[2] = any ? l : -1.f;
+                st[3] = acc_s[0][r][DH + 3];
+            }
+            if (whole) {
+                const float inv = any ? 1.f / l : 0.f;  // nothing held: zeros
+                sum *= inv;
+                *reinterpret_cast<uint2*>(a.o + head * DH + d) = make_uint2(
+                    f32_to_bf16(sum[0]) | static_cast<uint32_t>(f32_to_bf16(sum[1])) << 16,
+                    f32_to_bf16(sum[2]) | static_cast<uint32_t>(f32_to_bf16(sum[3])) << 16);
+                if (d == 0 && a.m_heads != nullptr) {
+                    a.m_heads[2 * head] = st[0] * inv;
+                    a.m_heads[2 * head + 1] = st[1] * inv;
+                }
+            } else {
+                *reinterpret_cast<f32x4_t*>(out + r * PITCH + d) = sum;
+                if (d == 0) *reinterpret_cast<f32x4_t*>(out + r * PITCH + DH) = st;
+            }
+        }
+
+        g += i1 - i0;
+        if (g == g_end) break;
+        first = false;
+        i0 = 0;
+        if (++hr == HR) {
+            hr = 0;
+            do {
+                ++b;
+                len = static_cast<int>(min(static_cast<int64_t>(max(seq_lens[b], 0)), cap));
+            } while (len == 0);  // g < g_end: there is another tile behind
+            nb = (len + T::TILE - 1) / T::TILE;
+        }
     }
+}
+
+// One workgroup per (sequence, query head): the partial results of the workers that share its tiles; zeros
+// for a sequence without tiles.
+template <int DH>
+__global__ void decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ seq_lens,
+                                   const float* __restrict__ part, const int64_t* __restrict__ plan) {
+    constexpr int PITCH = DH + 4, NF = DH / 4;
+    __shared__ __attribute__((aligned(16))) float red_s[DE_THREADS * 4];
+    __shared__ float max_s[DE_THREADS / kWave], stat_s[4];
+    const int b = static_cast<int>(blockIdx.x) / a.H, hq = static_cast<int>(blockIdx.x) % a.H;
+    const int hk = hq / a.group, r = hq % a.group;
+    const int hr = hk * a.rgroups + r / DE_ROWS, row = r % DE_ROWS;
+    const int64_t head = static_cast<int64_t>(b) * a.H + hq;
+    const int nb = seq_tiles(seq_lens[b], a.max_pages << a.page_shift, tile);
+    if (nb == 0) {
+        for (int d = threadIdx.x; d < DH; d += blockDim.x) a.o[head * DH + d] = 0;
+        if (threadIdx.x < 2 && a.m_heads != nullptr) a.m_heads[2 * head + threadIdx.x] = 0.f;
+        return;
+    }
+    const int64_t total = plan[0], g0 = plan[1 + b] + static_cast<int64_t>(hr) * nb;
+    auto worker = [&](int64_t g) { return static_cast<int>(((g + 1) * W - 1) / total); };
+    const int w0 = worker(g0), w1 = worker(g0 + nb - 1);
+    if (w0 == w1) return;
+    // a worker's second slot holds its last run, where that is not its first
+    auto slot = [&](int w) {
+        const bool second = w == w0 && total * w / W < g0;
+        return part + (static_cast<int64_t>(2 * w + (second ? 1 : 0))) * partial_floats(a.rows, DH) + row * PITCH;
+    };
+    float mt = -INFINITY;
+    for (int w = w0 + static_cast<int>(threadIdx.x); w <= w1; w += blockDim.x)
+        if (total * w / W < total * (w + 1) / W) mt = fmaxf(mt, slot(w)[DH + 3]);
+    mt = wave_max(mt);
+    if (lane_id() == 0) max_s[threadIdx.x / kWave] = mt;
     __syncthreads();
-    float M = -INFINITY, w[DE_WAVES], L = 0.f, any = 0.f;
-    for (int i = 0; i < DE_WAVES; ++i) M = fmaxf(M, stat_s[i][0]);
-    for (int i = 0; i < DE_WAVES; ++i) {
-        w[i] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat_s[i][0] - M);
-        L += w[i] * stat_s[i][1];
-        any += stat_s[i][4];
+    for (unsigned i = 0; i < blockDim.x / kWave; ++i) mt = fmaxf(mt, max_s[i]);
+    const float from = mt == -INFINITY ? 0.f : mt;
+    // thread (group, four dims): groups take the workers in turn
+    const int f = threadIdx.x % NF, grp = threadIdx.x / NF, ngrp = blockDim.x / NF;
+    f32x4_t sum{}, st{};
+    float seen = 0.f;
+    for (int w = w0 + grp; w <= w1; w += ngrp) {
+        if (total * w / W == total * (w + 1) / W) continue;  // a worker without tiles
+        const float* p = slot(w);
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + f * 4), y = *reinterpret_cast<const f32x4_t*>(p + DH);
+        const float wt = __builtin_amdgcn_exp2f(y[3] - from);
+        sum += x * wt;
+        if (y[2] != -1.f) {
+            st += f32x4_t{y[0], y[1], y[2], 0.f} * wt;
+            seen = 1.f;
+        }
     }
-    if (any == 0.f) L = 1.f;  // no key at all: zeros
-    const int64_t row = static_cast<int64_t>(b) * H + hq;
-    if (static_cast<int>(threadIdx.x) < DH) {
-        float r = 0.f;
-        for (int i = 0; i < DE_WAVES; ++i) r += w[i] * acc_s[i][threadIdx.x];
-        o[row * DH + threadIdx.x] = f32_to_bf16(r / L);
-    }
-    if (m_heads != nullptr && threadIdx.x < 2) {
-        float r = 0.f;
-        for (int i = 0; i < DE_WAVES; ++i) r += w[i] * stat_s[i][2 + threadIdx.x];
-        m_heads[2 * row + threadIdx.x] = r / L;
+    st[3] = seen;
+    *reinterpret_cast<f32x4_t*>(red_s + threadIdx.x * 4) = sum;
+    __syncthreads();
+    if (grp == 0)
+        for (int i = 1; i < ngrp; ++i) sum += *reinterpret_cast<const f32x4_t*>(red_s + (i * NF + f) * 4);
+    __syncthreads();
+    *reinterpret_cast<f32x4_t*>(red_s + threadIdx.x * 4) = st;
+    __syncthreads();
+    if (grp != 0) return;
+    for (int i = 1; i < ngrp; ++i) st += *reinterpret_cast<const f32x4_t*>(red_s + i * NF * 4);
+    const float inv = st[3] > 0.f ? 1.f / st[2] : 0.f;
+    sum *= inv;
+    *reinterpret_cast<uint2*>(a.o + head * DH + f * 4) =
+        make_uint2(f32_to_bf16(sum[0]) | static_cast<uint32_t>(f32_to_bf16(sum[1])) << 16,
+                   f32_to_bf16(sum[2]) | static_cast<uint32_t>(f32_to_bf16(sum[3])) << 16);
+    if (f == 0 && a.m_heads != nullptr) {
+        a.m_heads[2 * head] = st[0] * inv;
+        a.m_heads[2 * head + 1] = st[1] * inv;
     }
 }
 
 }  // namespace
 
-size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim) { return 0; }
+size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim) {
+    const int rows = H / n_kv_heads < DE_ROWS ? H / n_kv_heads : DE_ROWS;
+    return align_up(sizeof(float) * 2 * DE_WORKERS * partial_floats(rows, head_dim), 256) +
+           sizeof(int64_t) * (1 + static_cast<size_t>(n_seq));
+}
 
 hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, int H, float scale, void* o,
                          float* m_heads, void* ws, hipStream_t stream) {
+    DecodeArgs a;
+    a.n_pages = c.n_pages;
+    a.max_pages = c.max_pages;
+    a.q_stride = q_stride;
+    a.page_shift = c.page_shift;
+    a.n_kv_heads = c.n_kv_heads;
+    a.n_seq = c.n_seq;
+    a.H = H;
+    a.group = H / c.n_kv_heads;
+    a.rgroups = static_cast<int>(ceil_div(a.group, DE_ROWS));
+    a.rows = a.group < DE_ROWS ? a.group : DE_ROWS;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.k = static_cast<const uint8_t*>(c.k);
+    a.v = static_cast<const uint8_t*>(c.v);
+    a.k_scale = c.k_scale;
+    a.v_scale = c.v_scale;
+    a.m = c.m;
+    a.o = static_cast<uint16_t*>(o);
+    a.m_heads = m_heads;
+    float* part = static_cast<float*>(ws);
+    int64_t* plan = reinterpret_cast<int64_t*>(
+        static_cast<char*>(ws) + align_up(sizeof(float) * 2 * DE_WORKERS * partial_floats(a.rows, c.head_dim), 256));
+    int tile = 0;
     kv_dispatch(c, true, [&](auto dh, auto e4m3, auto) {
-        hipLaunchKernelGGL((decode_kernel<decltype(dh)::value, decltype(e4m3)::value>),
-                           dim3(static_cast<unsigned>(c.n_seq) * static_cast<unsigned>(H)), dim3(DE_THREADS), 0, stream,
-                           c, static_cast<const uint16_t*>(q), q_stride, H, scale * 1.4426950408889634f,
-                           static_cast<uint16_t*>(o), m_heads);
+        constexpr int NS = decltype(e4m3)::value ? 4 : 2;
+        tile = DecodeTile<decltype(dh)::value, decltype(e4m3)::value, NS>::TILE;
+        hipLaunchKernelGGL((decode_kernel<decltype(dh)::value, decltype(e4m3)::value, NS>), dim3(DE_WORKERS),
+                           dim3(DE_THREADS), 0, stream, a, static_cast<const uint16_t*>(q), c.block_table, c.seq_lens,
+                           part, plan);
     });
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    const unsigned heads = static_cast<unsigned>(c.n_seq) * static_cast<unsigned>(H);
+    if (c.head_dim == 128)
+        hipLaunchKernelGGL(decode_join_kernel<128>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, DE_WORKERS,
+                           c.seq_lens, part, plan);
+    else
+        hipLaunchKernelGGL(decode_join_kernel<64>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, DE_WORKERS,
+                           c.seq_lens, part, plan);
     return hipGetLastError();
 }
 
