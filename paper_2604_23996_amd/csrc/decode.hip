@@ -5,8 +5,8 @@
 // What bounds it is reading the cache once: 4 head_dim flops per key, value and query head, and at
 // most the 16 query heads of a group share a row. The work is cut evenly over a fixed number of
 // workgroups, whatever the sequences' lengths are: the tiles (DE_TILE keys of one sequence and
-// group) of all sequences stand in one row, and workgroup w takes tiles floor(w N / W) to
-// floor((w + 1) N / W). Lengths are only known on the device, so every workgroup counts the tiles
+// group) of all sequences stand in one row, and the workgroups take N / W of them
+// each, in order. Lengths are only known on the device, so every workgroup counts the tiles
 // itself. A run of tiles of one (sequence, group) that a workgroup holds whole is finished by it;
 // of one that is shared, every workgroup leaves its maximum, sums and unscaled output in the
 // workspace, and decode_join_kernel puts them together.
@@ -28,14 +28,23 @@ namespace {
 constexpr int DE_THREADS = 256;
 constexpr int DE_WAVES = DE_THREADS / kWave;
 constexpr int DE_ROWS = 16;        // query heads of a group that are worked on together
-constexpr int DE_WORKERS = 768;    // three workgroups per CU
+constexpr int DE_WORKERS = 512;    // two workgroups per CU
 constexpr float DE_LAZY = 8.f;     // the reference maximum moves when it is passed by this (log2)
 
-// Layout of the workspace: 2 partial results per worker, then the plan that the join reads.
-struct DecodePlan {
-    int64_t total;  // tiles of all sequences and groups
-};
+// Layout of the workspace: 2 partial results per worker, then the plan that the join reads: the
+// number of tiles of all sequences and groups, and the first tile of every sequence.
 __host__ __device__ constexpr int partial_floats(int rows, int dh) { return rows * (dh + 4); }
+
+// The even cut: the first total % W workers take one tile more than the others.
+struct Share {
+    int64_t quot, rem;
+    __device__ Share(int64_t total, int W) : quot(total / W), rem(total % W) {}
+    __device__ int64_t start(int w) const { return w * quot + (w < rem ? w : rem); }
+    __device__ int worker(int64_t g) const {  // of tile g
+        const int64_t more = rem * (quot + 1);
+        return static_cast<int>(g < more ? g / (quot + 1) : rem + (g - more) / quot);
+    }
+};
 
 struct DecodeArgs {
     int64_t n_pages, max_pages, q_stride;
@@ -93,19 +102,35 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p, int bytes)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, kBufferFlags);
 }
 
-template <int DH, bool E4M3, int NS>
-__global__ void __launch_bounds__(DE_THREADS)
+// The maximum of lanes l, l ^ 16, l ^ 32 and l ^ 48 (swaps of registers' rows: no trip through LDS).
+__device__ __forceinline__ float max_over_groups(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// acc += a b over one key per 16 lanes
+template <int QR>
+__device__ __forceinline__ f32x4_t product(float a, float b, f32x4_t acc) {
+    if constexpr (QR == 16) return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, acc, 0, 0, 0);
+}
+
+template <int DH, bool E4M3, int NS, int QR>
+__global__ void __launch_bounds__(DE_THREADS) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 2 : 3)))
 decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __restrict__ block_table,
               const int32_t* __restrict__ seq_lens, float* __restrict__ part, int64_t* __restrict__ plan) {
     using T = DecodeTile<DH, E4M3, NS>;
     constexpr int NQ = DH / 32;  // 32-wide slices of the logits' contraction
     constexpr int PITCH = DH + 4;
-    __shared__ __attribute__((aligned(16))) float acc_s[DE_WAVES][DE_ROWS][PITCH];
-    __shared__ float max_s[DE_WAVES][DE_ROWS];
+    constexpr int NP = DE_WAVES * 16 / QR;  // partial results of a run: per wave, with QR = 4 per wave and 16 lanes
+    __shared__ __attribute__((aligned(16))) float acc_s[NP][QR][PITCH];
+    __shared__ float max_s[DE_WAVES][QR];
     __shared__ int64_t scan_s[DE_WAVES];
     __shared__ int64_t found_s[2];
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave), lane = lane_id();
-    const int l16 = lane & 15, g4 = lane >> 4;
+    const int l16 = lane & 15, g4 = lane >> 4, lq = lane & (QR - 1);
     const int64_t cap = a.max_pages << a.page_shift;
     const int HR = a.n_kv_heads * a.rgroups;
     const int w = static_cast<int>(blockIdx.x), W = static_cast<int>(gridDim.x);
@@ -143,8 +168,9 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
     total *= HR;
     if (w == 0 && threadIdx.x == 0) plan[0] = total;
-    int64_t g = total * w / W;  // total < 2^31 tiles of 16 keys at least x 65535 heads: the product fits
-    const int64_t g_end = total * (w + 1) / W;
+    const Share share(total, W);
+    int64_t g = share.start(w);
+    const int64_t g_end = share.start(w + 1);
     if (g == g_end) return;
     {
         int64_t before = 0;
@@ -174,8 +200,8 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     // ---- runs of tiles
     while (true) {
         const int i1 = static_cast<int>(min(static_cast<int64_t>(nb), i0 + (g_end - g)));
-        const int hk = hr / a.rgroups, row0 = (hr % a.rgroups) * DE_ROWS;
-        const int rows = min(DE_ROWS, a.group - row0);
+        const int hk = hr / a.rgroups, row0 = (hr % a.rgroups) * QR;
+        const int rows = min(QR, a.group - row0);
         const int32_t* table = block_table + b * a.max_pages;
 
         // queries of the group as B fragments: slice c of lane l holds query l % 16, the dims of the
@@ -183,7 +209,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         bf16x8_t qf[NQ];
         {
             typedef int i32x4_u __attribute__((ext_vector_type(4), aligned(2)));
-            const uint16_t* qr = q + b * a.q_stride + static_cast<int64_t>(hk * a.group + row0 + min(l16, rows - 1)) * DH;
+            const uint16_t* qr = q + b * a.q_stride + static_cast<int64_t>(hk * a.group + row0 + min(lq, rows - 1)) * DH;
 #pragma unroll
             for (int c = 0; c < NQ; ++c) {
                 const int d = E4M3 ? 64 * (c >> 1) + 16 * g4 + 8 * (c & 1) : 32 * c + 8 * g4;
@@ -192,54 +218,54 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         }
 
         T t;
-        int page[NS], held[NS];
-        // pages of tile i's pieces of this wave, and how many of their rows are held (0: past the end, no page)
+        int entry[NS], held[NS];
+        int64_t row[NS], mrow[NS];
+        // Block table entries of tile i's pieces of this wave: loaded a tile before they are needed.
+        auto fetch = [&](int i) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                entry[s] = table[min((i * DE_WAVES + wave) * 16 * NS + 16 * s, len - 1) >> a.page_shift];
+        };
+        // From them: the pieces' first row in the pool's rows and scores, and how
+        // many of their rows are held (0: past the end, no page).
         auto pages = [&](int i) {
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
-                const bool in = i < i1 && pos < len;
-                const int p = in ? table[pos >> a.page_shift] : -1;
-                const bool ok = p >= 0 && p < a.n_pages;
-                page[s] = ok ? p : 0;
+                const bool ok = i < i1 && pos < len && entry[s] >= 0 && entry[s] < a.n_pages;
+                const int page = ok ? entry[s] : 0;
                 held[s] = ok ? min(16, len - pos) : 0;
+                const int slot = (pos & ((1 << a.page_shift) - 1));
+                row[s] = ((static_cast<int64_t>(page) * a.n_kv_heads + hk) << a.page_shift) + slot;
+                mrow[s] = ((static_cast<int64_t>(page) * 2) << a.page_shift) + slot;
             }
         };
-        // first row of piece s of tile i in the pool's rows of one head
-        auto row_of = [&](int i, int s) {
-            const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
-            return ((static_cast<int64_t>(page[s]) * a.n_kv_heads + hk) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-        };
         // rows that are not held are outside their buffer: they read as zeros and cost nothing
-        auto load_k = [&](int i) {
+        auto load_k = [&]() {
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                const int64_t row = row_of(i, s);
-                const auto r = rsrc(a.k + row * (DH * T::ES), held[s] * DH * T::ES);
+                const auto r = rsrc(a.k + row[s] * (DH * T::ES), held[s] * DH * T::ES);
 #pragma unroll
                 for (int c = 0; c < T::KL; ++c) {
                     const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, l16 * DH * T::ES + g4 * 16 + c * 64, 0, 0);
                     t.k[s][c] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
                 }
                 if constexpr (E4M3)
-                    t.ks[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale + row, (held[s] + 3) & ~3), g4 * 4, 0, 0));
+                    t.ks[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, 0));
                 t.nk[s] = held[s];
             }
         };
-        auto load_v_m = [&](int i) {
+        auto load_v_m = [&]() {
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                const int64_t row = row_of(i, s);
-                const auto r = rsrc(a.v + row * (DH * T::ES), held[s] * DH * T::ES);
+                const auto r = rsrc(a.v + row[s] * (DH * T::ES), held[s] * DH * T::ES);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) load_v<T::VB>(r, (g4 * 4 + e) * DH * T::ES + l16 * T::VB, t.v[s][e]);
                 if constexpr (E4M3)
-                    t.vs[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale + row, (held[s] + 3) & ~3), g4 * 4, 0, 0));
-                // vision scores for lanes l % 16 = 0, text for 1; the others read nothing
-                const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
-                const float* mp = a.m + ((static_cast<int64_t>(page[s]) * 2) << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-                const auto rm = rsrc(mp, a.m != nullptr && held[s] > 0 ? (4 << a.page_shift) + 64 : 0);
-                const auto x = __builtin_amdgcn_raw_buffer_load_b128(rm, l16 < 2 ? (l16 << (a.page_shift + 2)) + g4 * 16 : kOutOfRange, 0, 0);
+                    t.vs[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, 0));
+                // vision scores for lanes l % QR = 0, text for 1; the others read nothing
+                const auto rm = rsrc(a.m + mrow[s], a.m != nullptr && held[s] > 0 ? (4 << a.page_shift) + 64 : 0);
+                const auto x = __builtin_amdgcn_raw_buffer_load_b128(rm, lq < 2 ? (lq << (a.page_shift + 2)) + g4 * 16 : kOutOfRange, 0, 0);
                 t.m[s] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
                 t.nv[s] = held[s];
             }
@@ -251,11 +277,14 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         float m_run = -INFINITY;
         bool seen = false;
 
+        fetch(i0);
         pages(i0);
-        load_k(i0);
-        load_v_m(i0);
+        load_k();
+        // the keys' loads first: waiting for them leaves the values' in flight
+        __builtin_amdgcn_sched_barrier(0);
+        load_v_m();
+        fetch(i0 + 1);
         for (int i = i0; i < i1; ++i) {
-            pages(i + 1);
             // ---- logits, in units of log2
             f32x4_t s[NS];
             float mx = -INFINITY;
@@ -290,10 +319,12 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                 }
                 seen |= nk > 0;
             }
-            load_k(i + 1);
+            pages(i + 1);
+            load_k();
+            fetch(i + 2);
+            __builtin_amdgcn_sched_barrier(0);
             // ---- running maximum, moved lazily
-            mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+            mx = max_over_groups(mx);
             const bool grow = mx > m_run + DE_LAZY;
             if (__builtin_amdgcn_ballot_w64(grow) != 0) {
                 const float m_new = grow ? mx : m_run;
@@ -314,7 +345,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                     const float pr = __builtin_amdgcn_exp2f(s[p][e] - from);
                     float pv = pr;
                     if constexpr (E4M3) pv = in ? pr * __uint_as_float((static_cast<uint32_t>(t.vs[p]) >> (8 * e) & 0xffu) << 23) : 0.f;
-                    const float mc = l16 == 2 ? 1.f : in ? __int_as_float(t.m[p][e]) : 0.f;
+                    const float mc = lq == 2 ? 1.f : in ? __int_as_float(t.m[p][e]) : 0.f;
 #pragma unroll
                     for (int n = 0; n < T::VN; n += 2) {
                         float v0, v1;
@@ -328,33 +359,35 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                             v0 = __uint_as_float(y << 16);
                             v1 = __uint_as_float(y & 0xffff0000u);
                         }
-                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v0, pv, acc[n], 0, 0, 0);
-                        acc[n + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v1, pv, acc[n + 1], 0, 0, 0);
+                        acc[n] = product<QR>(v0, pv, acc[n]);
+                        acc[n + 1] = product<QR>(v1, pv, acc[n + 1]);
                     }
-                    acc[T::VN] = __builtin_amdgcn_mfma_f32_16x16x4f32(mc, pr, acc[T::VN], 0, 0, 0);
+                    acc[T::VN] = product<QR>(mc, pr, acc[T::VN]);
                 }
             }
-            load_v_m(i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v_m();
         }
 
         // ---- the four waves' results of this run: common maximum, then sums through LDS
         __syncthreads();  // the last run's are read
-        if (g4 == 0) max_s[wave][l16] = m_run;
+        if (lane < QR) max_s[wave][lane] = m_run;
         __syncthreads();
-        float mt = max_s[0][l16];
+        float mt = max_s[0][lq];
 #pragma unroll
-        for (int i = 1; i < DE_WAVES; ++i) mt = fmaxf(mt, max_s[i][l16]);
+        for (int i = 1; i < DE_WAVES; ++i) mt = fmaxf(mt, max_s[i][lq]);
         const float wt = __builtin_amdgcn_exp2f(m_run - (mt == -INFINITY ? 0.f : mt));
-        // element e of acc[n]: dim (4 (l / 16) + e) VN + n of query l % 16
-        float* row = acc_s[wave][l16];
+        // element e of acc[n]: dim (4 c + e) VN + n of query l % QR, c = l / 16 (QR = 16) or l % 16 / 4
+        const int c4 = QR == 16 ? g4 : l16 >> 2;
+        float* dst = acc_s[QR == 16 ? wave : wave * 4 + g4][lq];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int n = 0; n < T::VN; n += 4)
-                *reinterpret_cast<f32x4_t*>(row + (4 * g4 + e) * T::VN + n) =
+                *reinterpret_cast<f32x4_t*>(dst + (4 * c4 + e) * T::VN + n) =
                     f32x4_t{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]} * wt;
-        if (g4 == 0)  // vision, text, sum (-1: no key seen), maximum
-            *reinterpret_cast<f32x4_t*>(row + DH) =
+        if (c4 == 0)  // vision, text, sum (-1: no key seen), maximum
+            *reinterpret_cast<f32x4_t*>(dst + DH) =
                 f32x4_t{acc[T::VN][0] * wt, acc[T::VN][1] * wt, seen ? acc[T::VN][2] * wt : -1.f, mt};
         __syncthreads();
         const bool whole = i0 == 0 && i1 == nb;
@@ -365,7 +398,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             float l = 0.f;
             bool any = false;
 #pragma unroll
-            for (int i = 0; i < DE_WAVES; ++i) {
+            for (int i = 0; i < NP; ++i) {
                 sum += *reinterpret_cast<const f32x4_t*>(&acc_s[i][r][d]);
                 const float li = acc_s[i][r][DH + 2];
                 any |= li != -1.f;
@@ -375,7 +408,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             f32x4_t st{};
             if (d == 0) {
 #pragma unroll
-                for (int i = 0; i < DE_WAVES; ++i) {
+                for (int i = 0; i < NP; ++i) {
                     st[0] += acc_s[i][r][DH];
                     st[1] += acc_s[i][r][DH + 1];
                 }
@@ -423,7 +456,7 @@ __global__ void decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t*
     __shared__ float max_s[DE_THREADS / kWave], stat_s[4];
     const int b = static_cast<int>(blockIdx.x) / a.H, hq = static_cast<int>(blockIdx.x) % a.H;
     const int hk = hq / a.group, r = hq % a.group;
-    const int hr = hk * a.rgroups + r / DE_ROWS, row = r % DE_ROWS;
+    const int hr = hk * a.rgroups + r / a.rows, row = r % a.rows;
     const int64_t head = static_cast<int64_t>(b) * a.H + hq;
     const int nb = seq_tiles(seq_lens[b], a.max_pages << a.page_shift, tile);
     if (nb == 0) {
@@ -432,17 +465,17 @@ __global__ void decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t*
         return;
     }
     const int64_t total = plan[0], g0 = plan[1 + b] + static_cast<int64_t>(hr) * nb;
-    auto worker = [&](int64_t g) { return static_cast<int>(((g + 1) * W - 1) / total); };
-    const int w0 = worker(g0), w1 = worker(g0 + nb - 1);
+    const Share share(total, W);
+    const int w0 = share.worker(g0), w1 = share.worker(g0 + nb - 1);
     if (w0 == w1) return;
     // a worker's second slot holds its last run, where that is not its first
     auto slot = [&](int w) {
-        const bool second = w == w0 && total * w / W < g0;
+        const bool second = w == w0 && share.start(w) < g0;
         return part + (static_cast<int64_t>(2 * w + (second ? 1 : 0))) * partial_floats(a.rows, DH) + row * PITCH;
     };
     float mt = -INFINITY;
     for (int w = w0 + static_cast<int>(threadIdx.x); w <= w1; w += blockDim.x)
-        if (total * w / W < total * (w + 1) / W) mt = fmaxf(mt, slot(w)[DH + 3]);
+        mt = fmaxf(mt, slot(w)[DH + 3]);
     mt = wave_max(mt);
     if (lane_id() == 0) max_s[threadIdx.x / kWave] = mt;
     __syncthreads();
@@ -453,7 +486,6 @@ __global__ void decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t*
     f32x4_t sum{}, st{};
     float seen = 0.f;
     for (int w = w0 + grp; w <= w1; w += ngrp) {
-        if (total * w / W == total * (w + 1) / W) continue;  // a worker without tiles
         const float* p = slot(w);
         const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + f * 4), y = *reinterpret_cast<const f32x4_t*>(p + DH);
         const float wt = __builtin_amdgcn_exp2f(y[3] - from);
@@ -518,11 +550,12 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
         static_cast<char*>(ws) + align_up(sizeof(float) * 2 * DE_WORKERS * partial_floats(a.rows, c.head_dim), 256));
     int tile = 0;
     kv_dispatch(c, true, [&](auto dh, auto e4m3, auto) {
-        constexpr int NS = decltype(e4m3)::value ? 4 : 2;
-        tile = DecodeTile<decltype(dh)::value, decltype(e4m3)::value, NS>::TILE;
-        hipLaunchKernelGGL((decode_kernel<decltype(dh)::value, decltype(e4m3)::value, NS>), dim3(DE_WORKERS),
-                           dim3(DE_THREADS), 0, stream, a, static_cast<const uint16_t*>(q), c.block_table, c.seq_lens,
-                           part, plan);
+        constexpr int D = decltype(dh)::value, NS = decltype(e4m3)::value ? 4 : 2;
+        constexpr bool E = decltype(e4m3)::value;
+        tile = DecodeTile<D, E, NS>::TILE;
+        const auto kernel = a.group <= 4 ? decode_kernel<D, E, NS, 4> : decode_kernel<D, E, NS, 16>;
+        hipLaunchKernelGGL(kernel, dim3(DE_WORKERS), dim3(DE_THREADS), 0, stream, a, static_cast<const uint16_t*>(q),
+                           c.block_table, c.seq_lens, part, plan);
     });
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
