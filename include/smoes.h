@@ -739,7 +739,7 @@ enum smoes_kv_kind {
  *                    layer's input, or NULL for a layer that carries none
  * page_size: a power of two, 16 .. 4096; head_dim 64 or 128; 1 <= n_pages < 2^31.
  * block_table [n_seq, max_pages] int32: page of positions j page_size ... of each
- * sequence; max_pages * page_size < 2^31. An entry outside [0, n_pages) (e.g. -1)
+ * sequence; max_pages * page_size <= 2^30. An entry outside [0, n_pages) (e.g. -1)
  * is a page that is not held. Sequences may share pages that neither writes.
  * seq_lens [n_seq] int32: tokens of each sequence, those of the call included; one
  * below 0 counts as 0.

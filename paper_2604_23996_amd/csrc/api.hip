@@ -66,7 +66,7 @@ int check_kv(const smoes_kv_cache* c, int64_t max_pages, int n_seq, KvCacheArgs*
     if (c->n_pages < 1 || c->n_pages > INT32_MAX || n_seq < 0) return SMOES_ERR_SHAPE;
     if (c->page_size < 16 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0) return SMOES_ERR_SHAPE;
     if (c->n_kv_heads < 1 || c->n_kv_heads > 65535 || (c->head_dim != 64 && c->head_dim != 128)) return SMOES_ERR_SHAPE;
-    if (max_pages < 1 || max_pages > INT32_MAX / c->page_size) return SMOES_ERR_SHAPE;
+    if (max_pages < 1 || max_pages > (1 << 30) / c->page_size) return SMOES_ERR_SHAPE;
     out->n_pages = c->n_pages;
     out->max_pages = max_pages;
     out->page_shift = __builtin_ctz(static_cast<unsigned>(c->page_size));
@@ -414,7 +414,7 @@ size_t smoes_attention_decode_workspace_size(const smoes_kv_cache* cache, int n_
     if (check_kv(cache, 1, n_seq, &c) != SMOES_OK || n_heads < 1 || n_heads > 65535 ||
         (n_heads % cache->n_kv_heads) != 0)
         return 0;
-    return decode_workspace_bytes(n_seq, n_heads, cache->n_kv_heads, cache->head_dim) + 2 * kAlign;
+    return decode_workspace_bytes(n_seq, n_heads, cache->n_kv_heads, cache->head_dim, c.e4m3 != 0) + 2 * kAlign;
 }
 
 int smoes_attention_scores_decode(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
@@ -436,7 +436,7 @@ int smoes_attention_scores_decode(const smoes_kv_cache* cache, const int32_t* bl
     if (workspace == nullptr || workspace_bytes < smoes_attention_decode_workspace_size(cache, n_seq, n_heads))
         return SMOES_ERR_WORKSPACE;
     Carver w(workspace);
-    void* ws = w.take(decode_workspace_bytes(n_seq, n_heads, cache->n_kv_heads, cache->head_dim));
+    void* ws = w.take(decode_workspace_bytes(n_seq, n_heads, cache->n_kv_heads, cache->head_dim, c.e4m3 != 0));
     c.T = n_seq;
     c.block_table = block_table;
     c.seq_lens = seq_lens;

@@ -28,23 +28,14 @@ namespace {
 constexpr int DE_THREADS = 256;
 constexpr int DE_WAVES = DE_THREADS / kWave;
 constexpr int DE_ROWS = 16;        // query heads of a group that are worked on together
-constexpr int DE_WORKERS = 512;    // two workgroups per CU
+// Workgroups per CU and in all.
+__host__ __device__ constexpr int per_cu(bool e4m3) { return e4m3 ? 3 : 2; }
+__host__ __device__ constexpr int workers(bool e4m3) { return 256 * per_cu(e4m3); }
 constexpr float DE_LAZY = 8.f;     // the reference maximum moves when it is passed by this (log2)
 
 // Layout of the workspace: 2 partial results per worker, then the plan that the join reads: the
 // number of tiles of all sequences and groups, and the first tile of every sequence.
 __host__ __device__ constexpr int partial_floats(int rows, int dh) { return rows * (dh + 4); }
-
-// The even cut: the first total % W workers take one tile more than the others.
-struct Share {
-    int64_t quot, rem;
-    __device__ Share(int64_t total, int W) : quot(total / W), rem(total % W) {}
-    __device__ int64_t start(int w) const { return w * quot + (w < rem ? w : rem); }
-    __device__ int worker(int64_t g) const {  // of tile g
-        const int64_t more = rem * (quot + 1);
-        return static_cast<int>(g < more ? g / (quot + 1) : rem + (g - more) / quot);
-    }
-};
 
 struct DecodeArgs {
     int64_t n_pages, max_pages, q_stride;
@@ -59,10 +50,36 @@ struct DecodeArgs {
     float* m_heads;
 };
 
-__device__ __forceinline__ int seq_tiles(int len, int64_t cap, int tile) {
-    const int64_t n = min(static_cast<int64_t>(max(len, 0)), cap);
-    return static_cast<int>((n + tile - 1) / tile);
+// Four dims of a head's output, and with the first four its scores.
+__device__ __forceinline__ void store_row4(const DecodeArgs& a, int64_t head, int dh, int d, f32x4_t o, f32x4_t m) {
+    *reinterpret_cast<uint2*>(a.o + head * dh + d) =
+        make_uint2(f32_to_bf16(o[0]) | static_cast<uint32_t>(f32_to_bf16(o[1])) << 16,
+                   f32_to_bf16(o[2]) | static_cast<uint32_t>(f32_to_bf16(o[3])) << 16);
+    if (d == 0 && a.m_heads != nullptr) {
+        a.m_heads[2 * head] = m[0];
+        a.m_heads[2 * head + 1] = m[1];
+    }
 }
+
+// a / b of what nearly always fits 32 bits (a division of 64 bits is some 100 instructions more)
+__device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
+// The even cut: the first total % workers of them take one tile more than the others.
+struct Share {
+    int64_t quot, rem;
+    __device__ Share(int64_t total, int workers) : quot(div64(total, workers)), rem(total - quot * workers) {}
+    __device__ int64_t start(int w) const { return w * quot + (w < rem ? w : rem); }
+    __device__ int worker(int64_t g) const {  // of tile g
+        const int64_t more = rem * (quot + 1);
+        return static_cast<int>(g < more ? div64(g, quot + 1) : rem + div64(g - more, quot));
+    }
+};
+
+
+__device__ __forceinline__ int seq_len(int len, int cap) { return min(max(len, 0), cap); }
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -86,15 +103,15 @@ struct DecodeTile {
 template <int VB>
 __device__ __forceinline__ void load_v(__amdgpu_buffer_rsrc_t r, int off, int (&x)[VB / 4]) {
     if constexpr (VB == 16) {
-        const auto t = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+        const auto t = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kBufferNonTemporal);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = static_cast<int>(t[i]);
     } else if constexpr (VB == 8) {
-        const auto t = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+        const auto t = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kBufferNonTemporal);
         x[0] = static_cast<int>(t[0]);
         x[1] = static_cast<int>(t[1]);
     } else {
-        x[0] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+        x[0] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, kBufferNonTemporal));
     }
 }
 
@@ -118,7 +135,7 @@ __device__ __forceinline__ f32x4_t product(float a, float b, f32x4_t acc) {
 }
 
 template <int DH, bool E4M3, int NS, int QR>
-__global__ void __launch_bounds__(DE_THREADS) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 2 : 3)))
+__global__ void __launch_bounds__(DE_THREADS) __attribute__((amdgpu_waves_per_eu(per_cu(E4M3), DH == 128 ? per_cu(E4M3) : 4)))
 decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __restrict__ block_table,
               const int32_t* __restrict__ seq_lens, float* __restrict__ part, int64_t* __restrict__ plan) {
     using T = DecodeTile<DH, E4M3, NS>;
@@ -128,12 +145,13 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     __shared__ __attribute__((aligned(16))) float acc_s[NP][QR][PITCH];
     __shared__ float max_s[DE_WAVES][QR];
     __shared__ int64_t scan_s[DE_WAVES];
-    __shared__ int64_t found_s[2];
+    __shared__ int64_t in_seq_s;
+    __shared__ int found_s[2];
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave), lane = lane_id();
     const int l16 = lane & 15, g4 = lane >> 4, lq = lane & (QR - 1);
-    const int64_t cap = a.max_pages << a.page_shift;
+    const int cap = static_cast<int>(a.max_pages << a.page_shift);  // at most 2^30
     const int HR = a.n_kv_heads * a.rgroups;
-    const int w = static_cast<int>(blockIdx.x), W = static_cast<int>(gridDim.x);
+    const int w = static_cast<int>(blockIdx.x);
 
     // ---- the plan: all tiles, this workgroup's range, and where it starts
     // sum over 256 sequences at a time of their tiles: inclusive prefix of this thread's, and the whole
@@ -157,10 +175,14 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         return all;
     };
     int64_t total = 0, incl0 = 0;
-    int n0 = 0;
+    int n0 = 0, len0 = 0;  // of this thread's sequence
+    auto count = [&](int b) {
+        len0 = b < a.n_seq ? seq_len(seq_lens[b], cap) : 0;
+        n0 = (len0 + T::TILE - 1) / T::TILE;
+    };
     for (int b0 = 0; b0 < a.n_seq; b0 += DE_THREADS) {
         const int b = b0 + static_cast<int>(threadIdx.x);
-        n0 = b < a.n_seq ? seq_tiles(seq_lens[b], cap, T::TILE) : 0;
+        count(b);
         const int64_t before = total;
         total += scan(n0, incl0);
         // the join wants to know where every sequence's tiles start
@@ -168,7 +190,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
     total *= HR;
     if (w == 0 && threadIdx.x == 0) plan[0] = total;
-    const Share share(total, W);
+    const Share share(total, workers(E4M3));
     int64_t g = share.start(w);
     const int64_t g_end = share.start(w + 1);
     if (g == g_end) return;
@@ -177,113 +199,139 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         for (int b0 = 0; b0 < a.n_seq; b0 += DE_THREADS) {
             if (a.n_seq > DE_THREADS) {
                 const int b = b0 + static_cast<int>(threadIdx.x);
-                n0 = b < a.n_seq ? seq_tiles(seq_lens[b], cap, T::TILE) : 0;
+                count(b);
                 const int64_t all = scan(n0, incl0);
                 incl0 += before;
                 before += all;
             }
             if (n0 > 0 && (incl0 - n0) * HR <= g && g < incl0 * HR) {
                 found_s[0] = b0 + static_cast<int>(threadIdx.x);
-                found_s[1] = g - (incl0 - n0) * HR;
+                found_s[1] = len0;
+                in_seq_s = g - (incl0 - n0) * HR;
             }
         }
         __syncthreads();
     }
-    int b = __builtin_amdgcn_readfirstlane(static_cast<int>(found_s[0]));
-    int len = static_cast<int>(min(static_cast<int64_t>(max(seq_lens[b], 0)), cap));
-    int nb = (len + T::TILE - 1) / T::TILE;
-    const int64_t in_seq = found_s[1];
-    int hr = __builtin_amdgcn_readfirstlane(static_cast<int>(in_seq / nb));
-    int i0 = __builtin_amdgcn_readfirstlane(static_cast<int>(in_seq % nb));
+    // Where a run stands: a sequence, a (KV head, group of QR query heads) of it, a tile. Tiles are
+    // loaded ahead across runs: `ahead` is where block table entries are fetched from, two tiles
+    // before the products that need them; `at` where the products are.
+    struct Place {
+        int b, hr, i, len, nb;
+    };
+    Place at;
+    at.b = uniform_int(found_s[0]);
+    at.len = uniform_int(found_s[1]);
+    at.nb = (at.len + T::TILE - 1) / T::TILE;
+    at.hr = uniform_int(static_cast<int>(div64(in_seq_s, at.nb)));
+    at.i = uniform_int(static_cast<int>(in_seq_s - static_cast<int64_t>(at.hr) * at.nb));
+    auto next_group = [&](Place& p) {  // there has to be another tile behind
+        p.i = 0;
+        if (++p.hr < HR) return;
+        p.hr = 0;
+        do p.len = seq_len(seq_lens[++p.b], cap); while (p.len == 0);
+        p.nb = (p.len + T::TILE - 1) / T::TILE;
+    };
+    Place ahead = at;
+    int64_t to_fetch = g_end - g;  // tiles from `ahead` on
+
+    T t;
+    // Of the tile whose entries were fetched last: they, its KV head, its first key of this wave
+    // and that one's distance from the sequence's end (0 or less: nothing there).
+    int entry[NS], e_hk, e_pos, e_left;
+    auto fetch = [&]() {
+        const int32_t* table = block_table + ahead.b * a.max_pages;
+        e_pos = (ahead.i * DE_WAVES + wave) * 16 * NS;
+        e_left = to_fetch > 0 ? ahead.len - e_pos : 0;
+        e_hk = ahead.hr / a.rgroups;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) entry[s] = table[min(e_pos + 16 * s, ahead.len - 1) >> a.page_shift];
+        if (--to_fetch > 0 && ++ahead.i == ahead.nb) next_group(ahead);
+    };
+    // From them: the pieces' first row in the pool's rows and scores, and how many of their rows
+    // are held (0: past the end, no page).
+    int held[NS];
+    int64_t row[NS], mrow[NS];
+    auto pages = [&]() {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const bool ok = e_left > 16 * s && entry[s] >= 0 && entry[s] < a.n_pages;
+            const int64_t page = ok ? entry[s] : 0;
+            const int slot = (e_pos + 16 * s) & ((1 << a.page_shift) - 1);
+            held[s] = ok ? min(16, e_left - 16 * s) : 0;
+            row[s] = ((page * a.n_kv_heads + e_hk) << a.page_shift) + slot;
+            mrow[s] = ((page * 2) << a.page_shift) + slot;
+        }
+    };
+    // rows that are not held are outside their buffer: they read as zeros and cost nothing
+    auto load_k = [&]() {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const auto r = rsrc(a.k + row[s] * (DH * T::ES), held[s] * DH * T::ES);
+#pragma unroll
+            for (int c = 0; c < T::KL; ++c) {
+                const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, l16 * DH * T::ES + g4 * 16 + c * 64, 0, kBufferNonTemporal);
+                t.k[s][c] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
+            }
+            if constexpr (E4M3)
+                t.ks[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, kBufferNonTemporal));
+            t.nk[s] = held[s];
+        }
+    };
+    auto load_v_m = [&]() {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const auto r = rsrc(a.v + row[s] * (DH * T::ES), held[s] * DH * T::ES);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) load_v<T::VB>(r, (g4 * 4 + e) * DH * T::ES + l16 * T::VB, t.v[s][e]);
+            if constexpr (E4M3)
+                t.vs[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, kBufferNonTemporal));
+            // vision scores for lanes l % QR = 0, text for 1; the others read nothing
+            const auto rm = rsrc(a.m + mrow[s], a.m != nullptr && held[s] > 0 ? (4 << a.page_shift) + 64 : 0);
+            const auto x = __builtin_amdgcn_raw_buffer_load_b128(rm, lq < 2 ? (lq << (a.page_shift + 2)) + g4 * 16 : kOutOfRange, 0, kBufferNonTemporal);
+            t.m[s] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
+            t.nv[s] = held[s];
+        }
+    };
+
+    // Queries of `at`'s group as B fragments: slice c of lane l holds query l % QR, the dims of the key
+    // fragment it meets.
+    bf16x8_t qf[NQ];
+    auto load_q = [&](const Place& p) {
+        typedef int i32x4_u __attribute__((ext_vector_type(4), aligned(2)));
+        const int row0 = (p.hr % a.rgroups) * QR, head = (p.hr / a.rgroups) * a.group + row0 + min(lq, a.group - row0 - 1);
+        const uint16_t* qr = q + p.b * a.q_stride + static_cast<int64_t>(head) * DH;
+#pragma unroll
+        for (int c = 0; c < NQ; ++c) {
+            const int d = E4M3 ? 64 * (c >> 1) + 16 * g4 + 8 * (c & 1) : 32 * c + 8 * g4;
+            qf[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const i32x4_u*>(qr + d));
+        }
+    };
+
+    const int one = lq == 2 ? 0x3f800000 : 0;  // the third row of the scores' product: 1.0
+
+    fetch();
+    load_q(at);
+    pages();
+    load_k();
+    // the keys' loads first: waiting for them leaves the values' in flight
+    __builtin_amdgcn_sched_barrier(0);
+    load_v_m();
+    fetch();
     bool first = true;
 
     // ---- runs of tiles
     while (true) {
-        const int i1 = static_cast<int>(min(static_cast<int64_t>(nb), i0 + (g_end - g)));
-        const int hk = hr / a.rgroups, row0 = (hr % a.rgroups) * QR;
+        const int i0 = at.i, i1 = static_cast<int>(min(static_cast<int64_t>(at.nb), i0 + (g_end - g)));
+        const int hk = at.hr / a.rgroups, row0 = (at.hr % a.rgroups) * QR;
         const int rows = min(QR, a.group - row0);
-        const int32_t* table = block_table + b * a.max_pages;
-
-        // queries of the group as B fragments: slice c of lane l holds query l % 16, the dims of the
-        // key fragment it meets
-        bf16x8_t qf[NQ];
-        {
-            typedef int i32x4_u __attribute__((ext_vector_type(4), aligned(2)));
-            const uint16_t* qr = q + b * a.q_stride + static_cast<int64_t>(hk * a.group + row0 + min(lq, rows - 1)) * DH;
-#pragma unroll
-            for (int c = 0; c < NQ; ++c) {
-                const int d = E4M3 ? 64 * (c >> 1) + 16 * g4 + 8 * (c & 1) : 32 * c + 8 * g4;
-                qf[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const i32x4_u*>(qr + d));
-            }
-        }
-
-        T t;
-        int entry[NS], held[NS];
-        int64_t row[NS], mrow[NS];
-        // Block table entries of tile i's pieces of this wave: loaded a tile before they are needed.
-        auto fetch = [&](int i) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-                entry[s] = table[min((i * DE_WAVES + wave) * 16 * NS + 16 * s, len - 1) >> a.page_shift];
-        };
-        // From them: the pieces' first row in the pool's rows and scores, and how
-        // many of their rows are held (0: past the end, no page).
-        auto pages = [&](int i) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const int pos = (i * DE_WAVES + wave) * 16 * NS + 16 * s;
-                const bool ok = i < i1 && pos < len && entry[s] >= 0 && entry[s] < a.n_pages;
-                const int page = ok ? entry[s] : 0;
-                held[s] = ok ? min(16, len - pos) : 0;
-                const int slot = (pos & ((1 << a.page_shift) - 1));
-                row[s] = ((static_cast<int64_t>(page) * a.n_kv_heads + hk) << a.page_shift) + slot;
-                mrow[s] = ((static_cast<int64_t>(page) * 2) << a.page_shift) + slot;
-            }
-        };
-        // rows that are not held are outside their buffer: they read as zeros and cost nothing
-        auto load_k = [&]() {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const auto r = rsrc(a.k + row[s] * (DH * T::ES), held[s] * DH * T::ES);
-#pragma unroll
-                for (int c = 0; c < T::KL; ++c) {
-                    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, l16 * DH * T::ES + g4 * 16 + c * 64, 0, 0);
-                    t.k[s][c] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
-                }
-                if constexpr (E4M3)
-                    t.ks[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, 0));
-                t.nk[s] = held[s];
-            }
-        };
-        auto load_v_m = [&]() {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const auto r = rsrc(a.v + row[s] * (DH * T::ES), held[s] * DH * T::ES);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) load_v<T::VB>(r, (g4 * 4 + e) * DH * T::ES + l16 * T::VB, t.v[s][e]);
-                if constexpr (E4M3)
-                    t.vs[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, 0));
-                // vision scores for lanes l % QR = 0, text for 1; the others read nothing
-                const auto rm = rsrc(a.m + mrow[s], a.m != nullptr && held[s] > 0 ? (4 << a.page_shift) + 64 : 0);
-                const auto x = __builtin_amdgcn_raw_buffer_load_b128(rm, lq < 2 ? (lq << (a.page_shift + 2)) + g4 * 16 : kOutOfRange, 0, 0);
-                t.m[s] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
-                t.nv[s] = held[s];
-            }
-        };
-
+        const bool more = g + (i1 - i0) < g_end;
+        Place then = at;
         f32x4_t acc[T::VN + 1];
 #pragma unroll
         for (int n = 0; n <= T::VN; ++n) acc[n] = f32x4_t{};
         float m_run = -INFINITY;
         bool seen = false;
 
-        fetch(i0);
-        pages(i0);
-        load_k();
-        // the keys' loads first: waiting for them leaves the values' in flight
-        __builtin_amdgcn_sched_barrier(0);
-        load_v_m();
-        fetch(i0 + 1);
         for (int i = i0; i < i1; ++i) {
             // ---- logits, in units of log2
             f32x4_t s[NS];
@@ -319,9 +367,13 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                 }
                 seen |= nk > 0;
             }
-            pages(i + 1);
+            if (i + 1 == i1 && more) {
+                next_group(then);
+                load_q(then);
+            }
+            pages();
             load_k();
-            fetch(i + 2);
+            fetch();
             __builtin_amdgcn_sched_barrier(0);
             // ---- running maximum, moved lazily
             mx = max_over_groups(mx);
@@ -345,7 +397,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                     const float pr = __builtin_amdgcn_exp2f(s[p][e] - from);
                     float pv = pr;
                     if constexpr (E4M3) pv = in ? pr * __uint_as_float((static_cast<uint32_t>(t.vs[p]) >> (8 * e) & 0xffu) << 23) : 0.f;
-                    const float mc = lq == 2 ? 1.f : in ? __int_as_float(t.m[p][e]) : 0.f;
+                    const float mc = __int_as_float((t.m[p][e] & (in ? -1 : 0)) | one);
 #pragma unroll
                     for (int n = 0; n < T::VN; n += 2) {
                         float v0, v1;
@@ -390,7 +442,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             *reinterpret_cast<f32x4_t*>(dst + DH) =
                 f32x4_t{acc[T::VN][0] * wt, acc[T::VN][1] * wt, seen ? acc[T::VN][2] * wt : -1.f, mt};
         __syncthreads();
-        const bool whole = i0 == 0 && i1 == nb;
+        const bool whole = i0 == 0 && i1 == at.nb;
         float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH);
         for (int x = threadIdx.x; x < rows * (DH / 4); x += DE_THREADS) {
             const int r = x / (DH / 4), d = x % (DH / 4) * 4;
@@ -404,7 +456,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                 any |= li != -1.f;
                 l += li != -1.f ? li : 0.f;
             }
-            const int64_t head = static_cast<int64_t>(b) * a.H + hk * a.group + row0 + r;
+            const int64_t head = static_cast<int64_t>(at.b) * a.H + hk * a.group + row0 + r;
             f32x4_t st{};
             if (d == 0) {
 #pragma unroll
@@ -417,110 +469,108 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             }
             if (whole) {
                 const float inv = any ? 1.f / l : 0.f;  // nothing held: zeros
-                sum *= inv;
-                *reinterpret_cast<uint2*>(a.o + head * DH + d) = make_uint2(
-                    f32_to_bf16(sum[0]) | static_cast<uint32_t>(f32_to_bf16(sum[1])) << 16,
-                    f32_to_bf16(sum[2]) | static_cast<uint32_t>(f32_to_bf16(sum[3])) << 16);
-                if (d == 0 && a.m_heads != nullptr) {
-                    a.m_heads[2 * head] = st[0] * inv;
-                    a.m_heads[2 * head + 1] = st[1] * inv;
-                }
+                store_row4(a, head, DH, d, sum * inv, st * inv);
             } else {
                 *reinterpret_cast<f32x4_t*>(out + r * PITCH + d) = sum;
                 if (d == 0) *reinterpret_cast<f32x4_t*>(out + r * PITCH + DH) = st;
             }
         }
 
+        if (!more) break;
         g += i1 - i0;
-        if (g == g_end) break;
+        at = then;
         first = false;
-        i0 = 0;
-        if (++hr == HR) {
-            hr = 0;
-            do {
-                ++b;
-                len = static_cast<int>(min(static_cast<int64_t>(max(seq_lens[b], 0)), cap));
-            } while (len == 0);  // g < g_end: there is another tile behind
-            nb = (len + T::TILE - 1) / T::TILE;
-        }
     }
 }
 
 // One workgroup per (sequence, query head): the partial results of the workers that share its tiles; zeros
-// for a sequence without tiles.
+// for a sequence without tiles. Thread (group, four dims), the groups taking the workers in turn, a running
+// maximum and sums each; then the groups' results through LDS.
 template <int DH>
-__global__ void decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ seq_lens,
-                                   const float* __restrict__ part, const int64_t* __restrict__ plan) {
-    constexpr int PITCH = DH + 4, NF = DH / 4;
-    __shared__ __attribute__((aligned(16))) float red_s[DE_THREADS * 4];
-    __shared__ float max_s[DE_THREADS / kWave], stat_s[4];
+__global__ void __launch_bounds__(DE_THREADS)
+decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ seq_lens, const float* __restrict__ part,
+                   const int64_t* __restrict__ plan) {
+    constexpr int PITCH = DH + 4, NF = DH / 4, NG = DE_THREADS / NF, BATCH = 4;
+    __shared__ __attribute__((aligned(16))) float sum_s[NG][DH], stat_s[NG][4];
+    __shared__ float seen_s[NG];
     const int b = static_cast<int>(blockIdx.x) / a.H, hq = static_cast<int>(blockIdx.x) % a.H;
     const int hk = hq / a.group, r = hq % a.group;
     const int hr = hk * a.rgroups + r / a.rows, row = r % a.rows;
     const int64_t head = static_cast<int64_t>(b) * a.H + hq;
-    const int nb = seq_tiles(seq_lens[b], a.max_pages << a.page_shift, tile);
+    const int len = seq_len(seq_lens[b], static_cast<int>(a.max_pages << a.page_shift)), nb = (len + tile - 1) / tile;
+    const int64_t total = plan[0], seq0 = plan[1 + b];
     if (nb == 0) {
-        for (int d = threadIdx.x; d < DH; d += blockDim.x) a.o[head * DH + d] = 0;
+        for (int d = threadIdx.x; d < DH; d += DE_THREADS) a.o[head * DH + d] = 0;
         if (threadIdx.x < 2 && a.m_heads != nullptr) a.m_heads[2 * head + threadIdx.x] = 0.f;
         return;
     }
-    const int64_t total = plan[0], g0 = plan[1 + b] + static_cast<int64_t>(hr) * nb;
+    const int64_t g0 = seq0 + static_cast<int64_t>(hr) * nb;
     const Share share(total, W);
     const int w0 = share.worker(g0), w1 = share.worker(g0 + nb - 1);
     if (w0 == w1) return;
     // a worker's second slot holds its last run, where that is not its first
+    const int second = share.start(w0) < g0 ? 1 : 0;
     auto slot = [&](int w) {
-        const bool second = w == w0 && share.start(w) < g0;
-        return part + (static_cast<int64_t>(2 * w + (second ? 1 : 0))) * partial_floats(a.rows, DH) + row * PITCH;
+        return part + (2 * static_cast<int64_t>(w) + (w == w0 ? second : 0)) * partial_floats(a.rows, DH) + row * PITCH;
     };
-    float mt = -INFINITY;
-    for (int w = w0 + static_cast<int>(threadIdx.x); w <= w1; w += blockDim.x)
-        mt = fmaxf(mt, slot(w)[DH + 3]);
-    mt = wave_max(mt);
-    if (lane_id() == 0) max_s[threadIdx.x / kWave] = mt;
-    __syncthreads();
-    for (unsigned i = 0; i < blockDim.x / kWave; ++i) mt = fmaxf(mt, max_s[i]);
-    const float from = mt == -INFINITY ? 0.f : mt;
-    // thread (group, four dims): groups take the workers in turn
-    const int f = threadIdx.x % NF, grp = threadIdx.x / NF, ngrp = blockDim.x / NF;
+    const int f = threadIdx.x % NF, grp = threadIdx.x / NF;
+    float mt = -INFINITY, seen = 0.f;
     f32x4_t sum{}, st{};
-    float seen = 0.f;
-    for (int w = w0 + grp; w <= w1; w += ngrp) {
-        const float* p = slot(w);
-        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + f * 4), y = *reinterpret_cast<const f32x4_t*>(p + DH);
-        const float wt = __builtin_amdgcn_exp2f(y[3] - from);
-        sum += x * wt;
-        if (y[2] != -1.f) {
-            st += f32x4_t{y[0], y[1], y[2], 0.f} * wt;
-            seen = 1.f;
+    for (int w = w0 + grp; w <= w1; w += BATCH * NG) {
+        f32x4_t x[BATCH], y[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float* p = slot(min(w + i * NG, w1));
+            x[i] = *reinterpret_cast<const f32x4_t*>(p + f * 4);
+            y[i] = *reinterpret_cast<const f32x4_t*>(p + DH);
+        }
+        float top = mt;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) top = fmaxf(top, y[i][3]);
+        const float from = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(mt - from);
+        mt = top;
+        sum *= old;
+        st *= old;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (w + i * NG > w1) continue;
+            const float wt = __builtin_amdgcn_exp2f(y[i][3] - from);
+            sum += x[i] * wt;
+            if (y[i][2] != -1.f) {
+                st += f32x4_t{y[i][0], y[i][1], y[i][2], 0.f} * wt;
+                seen = 1.f;
+            }
         }
     }
-    st[3] = seen;
-    *reinterpret_cast<f32x4_t*>(red_s + threadIdx.x * 4) = sum;
-    __syncthreads();
-    if (grp == 0)
-        for (int i = 1; i < ngrp; ++i) sum += *reinterpret_cast<const f32x4_t*>(red_s + (i * NF + f) * 4);
-    __syncthreads();
-    *reinterpret_cast<f32x4_t*>(red_s + threadIdx.x * 4) = st;
+    *reinterpret_cast<f32x4_t*>(&sum_s[grp][f * 4]) = sum;
+    if (f == 0) {
+        *reinterpret_cast<f32x4_t*>(stat_s[grp]) = f32x4_t{st[0], st[1], st[2], mt};
+        seen_s[grp] = seen;
+    }
     __syncthreads();
     if (grp != 0) return;
-    for (int i = 1; i < ngrp; ++i) st += *reinterpret_cast<const f32x4_t*>(red_s + i * NF * 4);
-    const float inv = st[3] > 0.f ? 1.f / st[2] : 0.f;
-    sum *= inv;
-    *reinterpret_cast<uint2*>(a.o + head * DH + f * 4) =
-        make_uint2(f32_to_bf16(sum[0]) | static_cast<uint32_t>(f32_to_bf16(sum[1])) << 16,
-                   f32_to_bf16(sum[2]) | static_cast<uint32_t>(f32_to_bf16(sum[3])) << 16);
-    if (f == 0 && a.m_heads != nullptr) {
-        a.m_heads[2 * head] = st[0] * inv;
-        a.m_heads[2 * head + 1] = st[1] * inv;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) top = fmaxf(top, stat_s[i][3]);
+    const float from = top == -INFINITY ? 0.f : top;
+    sum = st = f32x4_t{};
+    seen = 0.f;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+        const float wt = __builtin_amdgcn_exp2f(stat_s[i][3] - from);
+        sum += *reinterpret_cast<const f32x4_t*>(&sum_s[i][f * 4]) * wt;
+        st += f32x4_t{stat_s[i][0], stat_s[i][1], stat_s[i][2], 0.f} * wt;
+        seen += seen_s[i];
     }
+    const float inv = seen > 0.f ? 1.f / st[2] : 0.f;
+    store_row4(a, head, DH, f * 4, sum * inv, st * inv);
 }
 
 }  // namespace
 
-size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim) {
+size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim, bool e4m3) {
     const int rows = H / n_kv_heads < DE_ROWS ? H / n_kv_heads : DE_ROWS;
-    return align_up(sizeof(float) * 2 * DE_WORKERS * partial_floats(rows, head_dim), 256) +
+    return align_up(sizeof(float) * 2 * workers(e4m3) * partial_floats(rows, head_dim), 256) +
            sizeof(int64_t) * (1 + static_cast<size_t>(n_seq));
 }
 
@@ -545,27 +595,28 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
     a.m = c.m;
     a.o = static_cast<uint16_t*>(o);
     a.m_heads = m_heads;
+    const int W = workers(c.e4m3 != 0);
     float* part = static_cast<float*>(ws);
     int64_t* plan = reinterpret_cast<int64_t*>(
-        static_cast<char*>(ws) + align_up(sizeof(float) * 2 * DE_WORKERS * partial_floats(a.rows, c.head_dim), 256));
+        static_cast<char*>(ws) + align_up(sizeof(float) * 2 * W * partial_floats(a.rows, c.head_dim), 256));
     int tile = 0;
     kv_dispatch(c, true, [&](auto dh, auto e4m3, auto) {
-        constexpr int D = decltype(dh)::value, NS = decltype(e4m3)::value ? 4 : 2;
+        constexpr int D = decltype(dh)::value, NS = 2;
         constexpr bool E = decltype(e4m3)::value;
         tile = DecodeTile<D, E, NS>::TILE;
         const auto kernel = a.group <= 4 ? decode_kernel<D, E, NS, 4> : decode_kernel<D, E, NS, 16>;
-        hipLaunchKernelGGL(kernel, dim3(DE_WORKERS), dim3(DE_THREADS), 0, stream, a, static_cast<const uint16_t*>(q),
+        hipLaunchKernelGGL(kernel, dim3(W), dim3(DE_THREADS), 0, stream, a, static_cast<const uint16_t*>(q),
                            c.block_table, c.seq_lens, part, plan);
     });
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     const unsigned heads = static_cast<unsigned>(c.n_seq) * static_cast<unsigned>(H);
     if (c.head_dim == 128)
-        hipLaunchKernelGGL(decode_join_kernel<128>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, DE_WORKERS,
-                           c.seq_lens, part, plan);
+        hipLaunchKernelGGL(decode_join_kernel<128>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, W, c.seq_lens,
+                           part, plan);
     else
-        hipLaunchKernelGGL(decode_join_kernel<64>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, DE_WORKERS,
-                           c.seq_lens, part, plan);
+        hipLaunchKernelGGL(decode_join_kernel<64>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, W, c.seq_lens,
+                           part, plan);
     return hipGetLastError();
 }
 

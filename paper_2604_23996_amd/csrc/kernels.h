@@ -254,7 +254,7 @@ void kv_dispatch(const KvCacheArgs& c, bool bf16, F go) {
 hipError_t launch_kv_write(const KvCacheArgs& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                            int act_dtype, const float* m_in, hipStream_t stream);
 hipError_t launch_kv_read(const KvCacheArgs& c, void* k, void* v, int out_dtype, float* m, hipStream_t stream);
-size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim);
+size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim, bool e4m3);
 hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, int H, float scale, void* o,
                          float* m_heads, void* ws, hipStream_t stream);
 
