@@ -153,6 +153,13 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     const int HR = a.n_kv_heads * a.rgroups;
     const int w = static_cast<int>(blockIdx.x);
 
+    // ---- zeros for the sequences without a token
+    for (int b = w; b < a.n_seq; b += workers(E4M3)) {
+        if (seq_lens[b] > 0) continue;
+        for (int x = threadIdx.x; x < a.H * (DH / 4); x += DE_THREADS)
+            store_row4(a, static_cast<int64_t>(b) * a.H + x / (DH / 4), DH, x % (DH / 4) * 4, f32x4_t{}, f32x4_t{});
+    }
+
     // ---- the plan: all tiles, this workgroup's range, and where it starts
     // sum over 256 sequences at a time of their tiles: inclusive prefix of this thread's, and the whole
     auto scan = [&](int n, int64_t& incl) {
@@ -483,8 +490,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
 }
 
-// One workgroup per (sequence, query head): the partial results of the workers that share its tiles; zeros
-// for a sequence without tiles. Thread (group, four dims), the groups taking the workers in turn, a running
+// One workgroup per (sequence, query head): the partial results of the workers that share its tiles. Thread (group, four dims), the groups taking the workers in turn, a running
 // maximum and sums each; then the groups' results through LDS.
 template <int DH>
 __global__ void __launch_bounds__(DE_THREADS)
@@ -499,11 +505,7 @@ decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ se
     const int64_t head = static_cast<int64_t>(b) * a.H + hq;
     const int len = seq_len(seq_lens[b], static_cast<int>(a.max_pages << a.page_shift)), nb = (len + tile - 1) / tile;
     const int64_t total = plan[0], seq0 = plan[1 + b];
-    if (nb == 0) {
-        for (int d = threadIdx.x; d < DH; d += DE_THREADS) a.o[head * DH + d] = 0;
-        if (threadIdx.x < 2 && a.m_heads != nullptr) a.m_heads[2 * head + threadIdx.x] = 0.f;
-        return;
-    }
+    if (nb <= 1) return;
     const int64_t g0 = seq0 + static_cast<int64_t>(hr) * nb;
     const Share share(total, W);
     const int w0 = share.worker(g0), w1 = share.worker(g0 + nb - 1);
@@ -609,7 +611,8 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
                            c.block_table, c.seq_lens, part, plan);
     });
     hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
+    // with one tile at most nothing is shared
+    if (err != hipSuccess || (c.max_pages << c.page_shift) <= tile) return err;
     const unsigned heads = static_cast<unsigned>(c.n_seq) * static_cast<unsigned>(H);
     if (c.head_dim == 128)
         hipLaunchKernelGGL(decode_join_kernel<128>, dim3(heads), dim3(DE_THREADS), 0, stream, a, tile, W, c.seq_lens,

@@ -393,51 +393,58 @@ def attn_score_update(x: torch.Tensor, x_attn: torch.Tensor, m_heads: torch.Tens
 # (a slice of a fused projection). Tensors have to lie on one GPU; the work runs there, on that
 # GPU's current stream, whichever GPU is current.
 
-def _gpu_of(*tensors: Optional[torch.Tensor]) -> torch.device:
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("libsmoes takes tensors on a GPU")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
+def _gpu_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The index of the GPU that holds all of these tensors."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("libsmoes takes tensors on a GPU")
+    for t in others:
+        if t is not None and t.get_device() != dev:
             raise ValueError("libsmoes takes tensors on one GPU")
     return dev
 
 
-def _launch(dev: torch.device, where: str, fn, *args) -> None:
-    if dev.index == torch.cuda.current_device():
-        status = fn(*args, _stream())
+def _launch(dev: int, where: str, fn, *args) -> None:
+    if dev == torch.cuda.current_device():
+        status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, _stream())
+            status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
     if status != SMOES_OK:
         raise SmoesError(status, where)
 
 
-def _heads(t: torch.Tensor, name: str, dtype=None, shape: Optional[Sequence[int]] = None) -> int:
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _heads(t: torch.Tensor, name: str, dtype, shape) -> int:
     """Checks a [tokens, heads, head_dim] tensor whose rows are dense inside a token; its token stride."""
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name}: expected {'[tokens, heads, head_dim]' if shape is None else tuple(shape)}, "
-                         f"got {tuple(t.shape)}")
-    if dtype is not None and t.dtype != dtype:
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    n, h, d = t.shape
+    n, h, d = shape
     s0, s1, s2 = t.stride()
-    if n * h * d > 0 and ((d > 1 and s2 != 1) or (h > 1 and s1 != d) or (n > 1 and s0 < h * d)):
-        raise ValueError(f"{name}: the heads of a token have to be dense (strides {t.stride()})")
-    return s0 if n > 1 else h * d
+    if (s2 == 1 or d == 1) and (s1 == d or h == 1) and (s0 >= h * d or n == 1) or n * h * d == 0:
+        return s0 if n > 1 else h * d
+    raise ValueError(f"{name}: the heads of a token have to be dense (strides {t.stride()})")
 
 
-def _array(t: Optional[torch.Tensor], name: str, dtype, shape: Sequence[int]) -> None:
+def _array(t: Optional[torch.Tensor], name: str, dtype, shape) -> None:
     if t is None:
         return
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected a dense {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _sizes(t: torch.Tensor, name: str, head_dim: int):
+    """Tokens and heads of a [tokens, heads, head_dim] tensor."""
+    if t.dim() != 3 or t.shape[2] != head_dim:
+        raise ValueError(f"{name}: expected [tokens, heads, {head_dim}], got {tuple(t.shape)}")
+    return t.shape[0], t.shape[1]
 
 
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -490,27 +497,26 @@ def rotary(plan: RotaryPlan, q: torch.Tensor, k: Optional[torch.Tensor] = None,
     """smoes_rotary_apply: q [T, H, head_dim] and k [T, Hkv, head_dim] at their int32 positions [T] (None:
     0 .. T - 1); backward=True takes the gradients of the rotated tensors to those before the rotation.
     Outputs are new dense tensors unless given (an input itself: in place). Returns (q_out, k_out or None)."""
-    dt, dh = _dtype_code(q), plan.spec.head_dim
-    q_stride = _heads(q, "q", None, (q.shape[0], q.shape[1], dh) if q.dim() == 3 else (-1, -1, dh))
-    T, H = q.shape[0], q.shape[1]
+    dt, dtype, dh = _dtype_code(q), q.dtype, plan.spec.head_dim
+    T, H = _sizes(q, "q", dh)
+    q_stride = _heads(q, "q", dtype, q.shape)
     if q_out is None:
-        q_out = torch.empty((T, H, dh), dtype=q.dtype, device=q.device)
-    qo_stride = _heads(q_out, "q_out", q.dtype, q.shape)
+        q_out = torch.empty((T, H, dh), dtype=dtype, device=q.device)
+    qo_stride = _heads(q_out, "q_out", dtype, q.shape)
     Hkv = k_stride = ko_stride = 0
     if k is not None:
-        Hkv = k.shape[1] if k.dim() == 3 else 0
-        k_stride = _heads(k, "k", q.dtype, (T, Hkv, dh))
+        Hkv = _sizes(k, "k", dh)[1]
+        k_stride = _heads(k, "k", dtype, (T, Hkv, dh))
         if k_out is None:
-            k_out = torch.empty((T, Hkv, dh), dtype=q.dtype, device=q.device)
-        ko_stride = _heads(k_out, "k_out", q.dtype, k.shape)
+            k_out = torch.empty((T, Hkv, dh), dtype=dtype, device=q.device)
+        ko_stride = _heads(k_out, "k_out", dtype, k.shape)
     elif k_out is not None:
         raise ValueError("k_out without k")
     _array(positions, "positions", torch.int32, (T,))
     dev = _gpu_of(plan.freqs, q, q_out, k, k_out, positions)
     _launch(dev, "smoes_rotary_apply", lib().smoes_rotary_apply, plan.desc, plan.freqs.data_ptr(), plan.amplitude,
-            None if positions is None else positions.data_ptr(), T, dt, int(backward), q.data_ptr(), q_stride, H,
-            q_out.data_ptr(), qo_stride, None if k is None else k.data_ptr(), k_stride, Hkv,
-            None if k is None else k_out.data_ptr(), ko_stride)
+            _ptr(positions), T, dt, int(backward), q.data_ptr(), q_stride, H, q_out.data_ptr(), qo_stride, _ptr(k),
+            k_stride, Hkv, _ptr(k_out), ko_stride)
     return q_out, k_out
 
 
@@ -546,37 +552,38 @@ class KVCache:
             self.v_scale = arr(v_scale, "v_scale", torch.uint8, shape[:3])
         if scores or m is not None:
             self.m = arr(m, "m", torch.float32, (n_pages, 2, page_size))
+        arrays = (self.k, self.v, self.k_scale, self.v_scale, self.m)
+        if any(t is not None and t.device != self.k.device for t in arrays):
+            raise ValueError("a cache lies on one device")
         self.desc = SmoesKvCache(n_pages, page_size, n_kv_heads, head_dim, KV_KINDS[kind],
                                  *(None if t is None else t.data_ptr()
-                                   for t in (self.k, self.v, self.k_scale, self.v_scale, self.m)))
-
-    def arrays(self):
-        return self.k, self.v, self.k_scale, self.v_scale, self.m
+                                   for t in arrays))
 
 
-def _kv_tables(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
-               sample_offsets: Optional[torch.Tensor]) -> int:
-    n_seq = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
+def _kv_tables(block_table: torch.Tensor, seq_lens: torch.Tensor, sample_offsets: Optional[torch.Tensor]):
+    """Sequences and pages of a row of the block table."""
+    if seq_lens.dim() != 1 or block_table.dim() != 2:
+        raise ValueError("seq_lens is [n_seq], block_table [n_seq, max_pages]")
+    n_seq, max_pages = seq_lens.shape[0], block_table.shape[1]
     _array(seq_lens, "seq_lens", torch.int32, (n_seq,))
-    _array(block_table, "block_table", torch.int32, (n_seq, block_table.shape[1] if block_table.dim() == 2 else -1))
+    _array(block_table, "block_table", torch.int32, (n_seq, max_pages))
     _array(sample_offsets, "sample_offsets", torch.int32, (n_seq + 1,))
-    return n_seq
+    return n_seq, max_pages
 
 
 def kv_write(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
              m_in: Optional[torch.Tensor] = None, sample_offsets: Optional[torch.Tensor] = None) -> None:
     """smoes_kv_write: append rows k, v [T, Hkv, head_dim] (bf16 or float32) and scores m_in [T, 2] behind what
     the sequences hold; seq_lens are the lengths with them. sample_offsets None: one token per sequence."""
-    n_seq = _kv_tables(cache, block_table, seq_lens, sample_offsets)
+    n_seq, max_pages = _kv_tables(block_table, seq_lens, sample_offsets)
     T = k.shape[0]
     shape = (T, cache.n_kv_heads, cache.head_dim)
-    k_stride, v_stride = _heads(k, "k", None, shape), _heads(v, "v", k.dtype, shape)
+    k_stride, v_stride = _heads(k, "k", k.dtype, shape), _heads(v, "v", k.dtype, shape)
     _array(m_in, "m_in", torch.float32, (T, 2))
-    dev = _gpu_of(*cache.arrays(), block_table, seq_lens, k, v, m_in, sample_offsets)
-    _launch(dev, "smoes_kv_write", lib().smoes_kv_write, cache.desc, block_table.data_ptr(), block_table.shape[1],
-            seq_lens.data_ptr(), n_seq, None if sample_offsets is None else sample_offsets.data_ptr(), T,
-            k.data_ptr(), k_stride, v.data_ptr(), v_stride, _dtype_code(k),
-            None if m_in is None else m_in.data_ptr())
+    dev = _gpu_of(cache.k, block_table, seq_lens, k, v, m_in, sample_offsets)
+    _launch(dev, "smoes_kv_write", lib().smoes_kv_write, cache.desc, block_table.data_ptr(), max_pages,
+            seq_lens.data_ptr(), n_seq, _ptr(sample_offsets), T, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
+            _dtype_code(k), _ptr(m_in))
 
 
 def kv_read(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
@@ -585,7 +592,7 @@ def kv_read(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
     """smoes_kv_read: the last tokens of every sequence as sample_offsets divides T rows among them (None: the
     last one of each), as dense (k, v [T, Hkv, head_dim], m [T, 2] or None). Outputs are written into k, v, m
     when given (rows behind the last sequence stay as they were), else new zeros of `dtype`."""
-    n_seq = _kv_tables(cache, block_table, seq_lens, sample_offsets)
+    n_seq, max_pages = _kv_tables(block_table, seq_lens, sample_offsets)
     if T is None:
         T = k.shape[0] if k is not None else v.shape[0] if v is not None else n_seq if sample_offsets is None else None
         if T is None:
@@ -600,10 +607,9 @@ def kv_read(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor,
     if m is None and cache.m is not None:
         m = torch.zeros((T, 2), dtype=torch.float32, device=cache.k.device)
     _array(m, "m", torch.float32, (T, 2))
-    dev = _gpu_of(*cache.arrays(), block_table, seq_lens, k, v, m, sample_offsets)
-    _launch(dev, "smoes_kv_read", lib().smoes_kv_read, cache.desc, block_table.data_ptr(), block_table.shape[1],
-            seq_lens.data_ptr(), n_seq, None if sample_offsets is None else sample_offsets.data_ptr(), T,
-            k.data_ptr(), v.data_ptr(), _dtype_code(k), None if m is None else m.data_ptr())
+    dev = _gpu_of(cache.k, block_table, seq_lens, k, v, m, sample_offsets)
+    _launch(dev, "smoes_kv_read", lib().smoes_kv_read, cache.desc, block_table.data_ptr(), max_pages,
+            seq_lens.data_ptr(), n_seq, _ptr(sample_offsets), T, k.data_ptr(), v.data_ptr(), _dtype_code(k), _ptr(m))
     return k, v, m
 
 
@@ -617,23 +623,23 @@ def attention_scores_decode(cache: KVCache, block_table: torch.Tensor, seq_lens:
     """smoes_attention_scores_decode: attention of one new token per sequence, q [n_seq, H, head_dim] (bf16), over
     the cache: (o [n_seq, H, head_dim] bf16, m_heads [n_seq, H, 2] float32 or None for a cache without scores).
     Calls that may overlap in time (other streams, graphs replayed beside each other) need a workspace each."""
-    n_seq = _kv_tables(cache, block_table, seq_lens, None)
-    H = q.shape[1] if q.dim() == 3 else 0
-    q_stride = _heads(q, "q", torch.bfloat16, (n_seq, H, cache.head_dim))
+    n_seq, max_pages = _kv_tables(block_table, seq_lens, None)
+    H = _sizes(q, "q", cache.head_dim)[1]
+    shape = (n_seq, H, cache.head_dim)
+    q_stride = _heads(q, "q", torch.bfloat16, shape)
     if o is None:
-        o = torch.empty((n_seq, H, cache.head_dim), dtype=torch.bfloat16, device=q.device)
+        o = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
     if m_heads is None and cache.m is not None:
         m_heads = torch.empty((n_seq, H, 2), dtype=torch.float32, device=q.device)
-    _array(o, "o", torch.bfloat16, (n_seq, H, cache.head_dim))
+    _array(o, "o", torch.bfloat16, shape)
     _array(m_heads, "m_heads", torch.float32, (n_seq, H, 2))
     if workspace is None:
         workspace = _workspace(attention_decode_workspace_bytes(cache, n_seq, H), q.device)
     _array(workspace, "workspace", torch.uint8, workspace.shape)
-    dev = _gpu_of(*cache.arrays(), block_table, seq_lens, q, o, m_heads, workspace)
+    dev = _gpu_of(cache.k, block_table, seq_lens, q, o, m_heads, workspace)
     _launch(dev, "smoes_attention_scores_decode", lib().smoes_attention_scores_decode, cache.desc,
-            block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(), n_seq, q.data_ptr(), q_stride, H,
-            scale, o.data_ptr(), None if m_heads is None else m_heads.data_ptr(), workspace.data_ptr(),
-            workspace.numel())
+            block_table.data_ptr(), max_pages, seq_lens.data_ptr(), n_seq, q.data_ptr(), q_stride, H, scale,
+            o.data_ptr(), _ptr(m_heads), workspace.data_ptr(), workspace.numel())
     return o, m_heads
 
 
