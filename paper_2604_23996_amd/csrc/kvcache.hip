@@ -16,25 +16,28 @@ namespace smoes {
 namespace {
 
 constexpr int KV_THREADS = 256;
+constexpr int KV_GROUPS = KV_THREADS / 16;  // rows at a time: 16 lanes each
+constexpr int KV_U = 4;                     // rows of a group in flight
+constexpr int KV_TOKENS = 32;               // most tokens of a workgroup
+constexpr int KV_SEQS = 1024;               // sample offsets that fit LDS
 
-// Where token t is kept: its page (< 0: nowhere) and slot, and the sequence it belongs to
-// (n_seq: a row behind the last sequence).
+// Where a token is kept: its page and slot; page < 0: nowhere; seq = n_seq: a row behind the last sequence.
 struct KvPlace {
     int page, slot, seq;
 };
-__device__ __forceinline__ KvPlace kv_place(const KvCacheArgs& c, int64_t t) {
+__device__ __forceinline__ KvPlace kv_place(const KvCacheArgs& c, const int32_t* offsets, int64_t t) {
     KvPlace p{-1, 0, c.n_seq};
     int b = static_cast<int>(t), n = 1, j = 0;
-    if (c.sample_offsets != nullptr) {
-        if (t >= c.sample_offsets[c.n_seq] || t < c.sample_offsets[0]) return p;
+    if (offsets != nullptr) {
+        if (t >= offsets[c.n_seq] || t < offsets[0]) return p;
         int lo = 0, hi = c.n_seq - 1;
         while (lo < hi) {  // the last sequence that starts at t or before
             const int mid = (lo + hi + 1) >> 1;
-            if (c.sample_offsets[mid] <= t) lo = mid; else hi = mid - 1;
+            if (offsets[mid] <= t) lo = mid; else hi = mid - 1;
         }
         b = lo;
-        const int start = c.sample_offsets[b];
-        n = c.sample_offsets[b + 1] - start;
+        const int start = offsets[b];
+        n = offsets[b + 1] - start;
         j = static_cast<int>(t) - start;
     }
     p.seq = b;
@@ -47,127 +50,246 @@ __device__ __forceinline__ KvPlace kv_place(const KvCacheArgs& c, int64_t t) {
     return p;
 }
 
+// The places of a workgroup's tokens t0 .. t0 + nt - 1, a thread each, into LDS. The search of the
+// sequence goes over a copy of the offsets there: one load instead of a chain of them.
+struct KvPlaces {
+    KvPlace at[KV_TOKENS];
+    int offsets[KV_SEQS];
+};
+__device__ __forceinline__ void find_places(const KvCacheArgs& c, int64_t t0, int nt, KvPlaces& s) {
+    const bool copy = c.sample_offsets != nullptr && c.n_seq < KV_SEQS;
+    if (copy) {
+        for (int i = threadIdx.x; i <= c.n_seq; i += KV_THREADS) s.offsets[i] = c.sample_offsets[i];
+        __syncthreads();
+    }
+    if (static_cast<int>(threadIdx.x) < nt)
+        s.at[threadIdx.x] = kv_place(c, copy ? s.offsets : c.sample_offsets, t0 + threadIdx.x);
+    __syncthreads();
+}
+
 // Exponent e of a row's scale 2^e, from the largest magnitude of its finite values:
 // the smallest e >= -117 with top <= 448 * 2^e; 0 for a row of zeros.
-__device__ __forceinline__ int scale_exponent(float top) {
-    if (top == 0.f) return 0;
-    const uint32_t u = __float_as_uint(top);
+__device__ __forceinline__ int scale_exponent(uint32_t top) {
+    if (top == 0) return 0;
     // top = 1.f * 2^(E - 127): top <= 1.75 * 2^8 * 2^e for e = E - 135, or one more beyond 1.75
-    const int e = static_cast<int>(u >> 23) - 135 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    const int e = static_cast<int>(top >> 23) - 135 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
     return e < -117 ? -117 : e;
 }
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 
 // x / 2^e as an e4m3 code, rounded to nearest even; an infinity has no code and becomes NaN. 1.875 2^127 is
 // the last code times scale below infinity: of a row whose scale is 2^120 nothing may be rounded to 256.
-__device__ __forceinline__ uint8_t to_e4m3(float x, int e) {
+__device__ __forceinline__ uint32_t to_e4m3(float x, int e) {
     if (!(fabsf(x) < INFINITY)) return 0x7f | (__float_as_uint(x) >> 31 << 7);
     const float y = fminf(fmaxf(x, -0x1.ep127f), 0x1.ep127f) * exp2_int(-e);
-    return static_cast<uint8_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xff);
-}
-__device__ __forceinline__ float from_e4m3(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8(c, 0); }
-
-template <bool BF16>
-__device__ __forceinline__ float ld1(const void* p, int64_t i) {
-    if constexpr (BF16) return bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-    else return static_cast<const float*>(p)[i];
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false)) & 0xffu;
 }
 
-// One wave per row: (token, KV head, keys or values).
-template <int DH, bool E4M3, bool IN_BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, const void* __restrict__ k, int64_t k_stride,
-                                                              const void* __restrict__ v, int64_t v_stride,
-                                                              const float* __restrict__ m_in) {
-    constexpr int N = DH / kWave;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (KV_THREADS / kWave) + threadIdx.x / kWave;
-    if (row >= c.T * c.n_kv_heads * 2) return;
-    const int lane = lane_id();
-    const int which = static_cast<int>(row & 1), h = static_cast<int>((row >> 1) % c.n_kv_heads);
-    const int64_t t = (row >> 1) / c.n_kv_heads;
-    const KvPlace p = kv_place(c, t);
-    if (p.page < 0) return;
-    const void* x = which ? v : k;
-    const int64_t at = t * (which ? v_stride : k_stride) + static_cast<int64_t>(h) * DH;
-    const int64_t slot = ((static_cast<int64_t>(p.page) * c.n_kv_heads + h) << c.page_shift) + p.slot;
-    float e[N];
+// N consecutive values at any element (N * size is 8, 16 or 32 bytes).
+template <bool BF16, int N>
+__device__ __forceinline__ void load_row(const void* base, int64_t i, float (&x)[N]) {
+    if constexpr (BF16) {
+        typedef uint32_t vec __attribute__((ext_vector_type(N / 2), aligned(2)));
+        const vec r = *reinterpret_cast<const vec*>(static_cast<const uint16_t*>(base) + i);
 #pragma unroll
-    for (int i = 0; i < N; ++i) e[i] = ld1<IN_BF16>(x, at + lane * N + i);
-    if constexpr (E4M3) {
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(e[i]) < INFINITY ? fabsf(e[i]) : 0.f);
-        const int ex = scale_exponent(wave_max_u(top));
-        uint8_t* out = static_cast<uint8_t*>(which ? c.v : c.k) + slot * DH + lane * N;
-#pragma unroll
-        for (int i = 0; i < N; ++i) out[i] = to_e4m3(e[i], ex);
-        if (lane == 0) (which ? c.v_scale : c.k_scale)[slot] = static_cast<uint8_t>(ex + 127);
+        for (int e = 0; e < N; ++e) x[e] = __uint_as_float(e % 2 ? r[e / 2] & 0xffff0000u : r[e / 2] << 16);
     } else {
-        uint16_t* out = static_cast<uint16_t*>(which ? c.v : c.k) + slot * DH + lane * N;
+        typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-        for (int i = 0; i < N; ++i) out[i] = f32_to_bf16(e[i]);
+        for (int v = 0; v < N / 4; ++v) {
+            const vec r = *reinterpret_cast<const vec*>(static_cast<const float*>(base) + i + 4 * v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * v + e] = r[e];
+        }
     }
-    if (m_in != nullptr && h == 0 && lane == 0)
-        c.m[((static_cast<int64_t>(p.page) * 2 + which) << c.page_shift) + p.slot] = m_in[2 * t + which];
+}
+template <int N>
+__device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[N]) {
+    typedef uint32_t vec __attribute__((ext_vector_type(N)));
+    vec r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = w[i];
+    *static_cast<vec*>(p) = r;
+}
+
+// A workgroup takes `tokens` tokens; 16 lanes a row of one token, (keys or values) and KV head, in this
+// order, so that what is read lies together. Bound by reading every value and writing its cached form.
+template <int DH, bool E4M3, bool IN_BF16>
+__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int tokens, const void* __restrict__ k,
+                                                              int64_t k_stride, const void* __restrict__ v,
+                                                              int64_t v_stride, const float* __restrict__ m_in) {
+    constexpr int N = DH / 16;
+    __shared__ KvPlaces places;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * tokens;
+    const int nt = static_cast<int>(min(static_cast<int64_t>(tokens), c.T - t0));
+    const int per_token = 2 * c.n_kv_heads, rows = nt * per_token;
+    const int l16 = threadIdx.x & 15;
+    float x[KV_U][N];
+    auto load = [&](int r0) {
+#pragma unroll
+        for (int u = 0; u < KV_U; ++u) {
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const bool is_v = j >= c.n_kv_heads;
+            const int h = is_v ? j - c.n_kv_heads : j;
+            load_row<IN_BF16, N>(is_v ? v : k, (t0 + t) * (is_v ? v_stride : k_stride) + static_cast<int64_t>(h) * DH + l16 * N, x[u]);
+        }
+    };
+    const int g = threadIdx.x / 16;
+    load(g);
+    find_places(c, t0, nt, places);
+    for (int r0 = g;;) {
+#pragma unroll
+        for (int u = 0; u < KV_U; ++u) {
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const bool is_v = j >= c.n_kv_heads;
+            const int h = is_v ? j - c.n_kv_heads : j;
+            const KvPlace p = places.at[t];
+            const bool keep = r0 + u * KV_GROUPS < rows && p.page >= 0;
+            const int64_t slot = ((static_cast<int64_t>(p.page) * c.n_kv_heads + h) << c.page_shift) + p.slot;
+            if constexpr (E4M3) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(x[u][e]) & 0x7fffffffu);
+                top = row_allreduce(static_cast<int>(top), [](int a, int b) { return max(a, b); });
+                const bool plain = top < 0x7f000000u;  // no infinity, NaN or value that might be rounded to one
+                uint32_t w[N / 4];
+                int ex = scale_exponent(top);
+                if (__builtin_amdgcn_ballot_w64(!plain) != 0) {
+                    top = 0;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const uint32_t a = __float_as_uint(x[u][e]) & 0x7fffffffu;
+                        top = a < 0x7f800000u ? max(top, a) : top;
+                    }
+                    top = row_allreduce(static_cast<int>(top), [](int a, int b) { return max(a, b); });
+                    ex = scale_exponent(top);
+#pragma unroll
+                    for (int e = 0; e < N; e += 4)
+                        w[e / 4] = to_e4m3(x[u][e], ex) | to_e4m3(x[u][e + 1], ex) << 8 | to_e4m3(x[u][e + 2], ex) << 16 |
+                                   to_e4m3(x[u][e + 3], ex) << 24;
+                } else {
+                    const float f = exp2_int(-ex);
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) {
+                        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[u][e] * f, x[u][e + 1] * f, 0, false);
+                        w[e / 4] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(x[u][e + 2] * f, x[u][e + 3] * f, lo, true));
+                    }
+                }
+                if (keep) {
+                    store_words(static_cast<uint8_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
+                    if (l16 == 0) (is_v ? c.v_scale : c.k_scale)[slot] = static_cast<uint8_t>(ex + 127);
+                }
+            } else {
+                uint32_t w[N / 2];
+#pragma unroll
+                for (int e = 0; e < N; e += 2)
+                    w[e / 2] = f32_to_bf16(x[u][e]) | static_cast<uint32_t>(f32_to_bf16(x[u][e + 1])) << 16;
+                if (keep) store_words(static_cast<uint16_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
+            }
+        }
+        r0 += KV_U * KV_GROUPS;
+        if (r0 - g >= rows) break;
+        load(r0);
+    }
+    if (m_in != nullptr && static_cast<int>(threadIdx.x) < 2 * nt) {
+        const KvPlace p = places.at[threadIdx.x / 2];
+        if (p.page >= 0)
+            c.m[((static_cast<int64_t>(p.page) * 2 + (threadIdx.x & 1)) << c.page_shift) + p.slot] = m_in[2 * t0 + threadIdx.x];
+    }
 }
 
 template <int DH, bool E4M3, bool OUT_BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, void* __restrict__ k, void* __restrict__ v,
-                                                             float* __restrict__ m) {
-    constexpr int N = DH / kWave;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (KV_THREADS / kWave) + threadIdx.x / kWave;
-    if (row >= c.T * c.n_kv_heads * 2) return;
-    const int lane = lane_id();
-    const int which = static_cast<int>(row & 1), h = static_cast<int>((row >> 1) % c.n_kv_heads);
-    const int64_t t = (row >> 1) / c.n_kv_heads;
-    const KvPlace p = kv_place(c, t);
-    if (p.seq >= c.n_seq) return;
-    const int64_t slot = ((static_cast<int64_t>(p.page) * c.n_kv_heads + h) << c.page_shift) + p.slot;
-    float e[N] = {};
-    if (p.page >= 0) {
+__global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int tokens, void* __restrict__ k,
+                                                             void* __restrict__ v, float* __restrict__ m) {
+    constexpr int N = DH / 16, W = E4M3 ? N / 4 : N / 2;  // words of a lane
+    typedef uint32_t vec __attribute__((ext_vector_type(W)));
+    __shared__ KvPlaces places;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * tokens;
+    const int nt = static_cast<int>(min(static_cast<int64_t>(tokens), c.T - t0));
+    const int per_token = 2 * c.n_kv_heads, rows = nt * per_token;
+    const int l16 = threadIdx.x & 15, g = threadIdx.x / 16;
+    find_places(c, t0, nt, places);
+    for (int r0 = g; r0 - g < rows; r0 += KV_U * KV_GROUPS) {
+        vec x[KV_U];
+        float f[KV_U];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (E4M3)
-                e[i] = from_e4m3(static_cast<const uint8_t*>(which ? c.v : c.k)[slot * DH + lane * N + i]) *
-                       exp2_int((which ? c.v_scale : c.k_scale)[slot] - 127);
-            else
-                e[i] = bf16_to_f32(static_cast<const uint16_t*>(which ? c.v : c.k)[slot * DH + lane * N + i]);
+        for (int u = 0; u < KV_U; ++u) {
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const bool is_v = j >= c.n_kv_heads;
+            const int h = is_v ? j - c.n_kv_heads : j;
+            const KvPlace p = places.at[t];
+            const int64_t slot = ((static_cast<int64_t>(max(p.page, 0)) * c.n_kv_heads + h) << c.page_shift) + p.slot;
+            x[u] = *reinterpret_cast<const vec*>(static_cast<const uint8_t*>(is_v ? c.v : c.k) + slot * (DH * (E4M3 ? 1 : 2)) + l16 * (W * 4));
+            if constexpr (E4M3) f[u] = __uint_as_float(static_cast<uint32_t>((is_v ? c.v_scale : c.k_scale)[slot]) << 23);
+        }
+#pragma unroll
+        for (int u = 0; u < KV_U; ++u) {
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const bool is_v = j >= c.n_kv_heads;
+            const int h = is_v ? j - c.n_kv_heads : j;
+            const KvPlace p = places.at[t];
+            void* y = is_v ? v : k;
+            if (r0 + u * KV_GROUPS >= rows || p.seq >= c.n_seq || y == nullptr) continue;
+            float e[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (E4M3) {
+                    const auto q = i % 4 < 2 ? __builtin_amdgcn_cvt_pk_f32_fp8(x[u][i / 4], false) : __builtin_amdgcn_cvt_pk_f32_fp8(x[u][i / 4], true);
+                    e[i] = q[i % 2] * f[u];
+                } else {
+                    e[i] = __uint_as_float(i % 2 ? x[u][i / 2] & 0xffff0000u : x[u][i / 2] << 16);
+                }
+                if (p.page < 0) e[i] = 0.f;
+            }
+            const int64_t at = ((t0 + t) * c.n_kv_heads + h) * DH + l16 * N;
+            if constexpr (OUT_BF16) {
+                uint32_t w[N / 2];
+#pragma unroll
+                for (int i = 0; i < N; i += 2) w[i / 2] = f32_to_bf16(e[i]) | static_cast<uint32_t>(f32_to_bf16(e[i + 1])) << 16;
+                store_words(static_cast<uint16_t*>(y) + at, w);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; i += 4) {
+                    const uint32_t w[4] = {__float_as_uint(e[i]), __float_as_uint(e[i + 1]), __float_as_uint(e[i + 2]), __float_as_uint(e[i + 3])};
+                    store_words(static_cast<float*>(y) + at + i, w);
+                }
+            }
         }
     }
-    void* y = which ? v : k;
-    if (y != nullptr) {
-        const int64_t at = (t * c.n_kv_heads + h) * DH + lane * N;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (OUT_BF16) static_cast<uint16_t*>(y)[at + i] = f32_to_bf16(e[i]);
-            else static_cast<float*>(y)[at + i] = e[i];
-        }
+    if (m != nullptr && static_cast<int>(threadIdx.x) < 2 * nt) {
+        const KvPlace p = places.at[threadIdx.x / 2];
+        if (p.seq < c.n_seq)
+            m[2 * t0 + threadIdx.x] = p.page < 0 ? 0.f : c.m[((static_cast<int64_t>(p.page) * 2 + (threadIdx.x & 1)) << c.page_shift) + p.slot];
     }
-    if (m != nullptr && h == 0 && lane == 0)
-        m[2 * t + which] = p.page < 0 ? 0.f : c.m[((static_cast<int64_t>(p.page) * 2 + which) << c.page_shift) + p.slot];
 }
 
-unsigned row_blocks(const KvCacheArgs& c) {
-    return static_cast<unsigned>(ceil_div(c.T * c.n_kv_heads * 2, KV_THREADS / kWave));
+// Tokens of a workgroup: four rows for every 16 lanes, but no fewer than 1024 workgroups for it.
+int tokens_of(const KvCacheArgs& c) {
+    int64_t n = ceil_div(KV_GROUPS * KV_U, 2 * c.n_kv_heads);
+    if (n > c.T / 1024) n = c.T / 1024;
+    if (n > KV_TOKENS) n = KV_TOKENS;
+    return n < 1 ? 1 : static_cast<int>(n);
 }
 
 }  // namespace
 
 hipError_t launch_kv_write(const KvCacheArgs& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                            int act_dtype, const float* m_in, hipStream_t stream) {
-    auto go = [&](auto dh, auto e4m3, auto bf16) {
+    const int n = tokens_of(c);
+    kv_dispatch(c, act_dtype == 1, [&](auto dh, auto e4m3, auto bf16) {
         hipLaunchKernelGGL((kv_write_kernel<decltype(dh)::value, decltype(e4m3)::value, decltype(bf16)::value>),
-                           dim3(row_blocks(c)), dim3(KV_THREADS), 0, stream, c, k, k_stride, v, v_stride, m_in);
-    };
-    kv_dispatch(c, act_dtype == 1, go);
+                           dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n, k, k_stride,
+                           v, v_stride, m_in);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvCacheArgs& c, void* k, void* v, int out_dtype, float* m, hipStream_t stream) {
-    auto go = [&](auto dh, auto e4m3, auto bf16) {
+    const int n = tokens_of(c);
+    kv_dispatch(c, out_dtype == 1, [&](auto dh, auto e4m3, auto bf16) {
         hipLaunchKernelGGL((kv_read_kernel<decltype(dh)::value, decltype(e4m3)::value, decltype(bf16)::value>),
-                           dim3(row_blocks(c)), dim3(KV_THREADS), 0, stream, c, k, v, m);
-    };
-    kv_dispatch(c, out_dtype == 1, go);
+                           dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n, k, v, m);
+    });
     return hipGetLastError();
 }
 
