@@ -263,9 +263,11 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
     }
 }
 
-// Tokens of a workgroup: four rows for every 16 lanes, but no fewer than 1024 workgroups for it.
-int tokens_of(const KvCacheArgs& c) {
-    int64_t n = ceil_div(KV_GROUPS * KV_U, 2 * c.n_kv_heads);
+// Tokens of a workgroup: `rows` for every 16 lanes, but no fewer than 1024 workgroups for it. Writing 16384
+// tokens x 8 heads of 128 in e4m3 takes 28.9 us with 4 rows and 26.9 with 16 (longer pieces of a page
+// at a time), reading 27.7 and 28.7.
+int tokens_of(const KvCacheArgs& c, int rows) {
+    int64_t n = ceil_div(KV_GROUPS * rows, 2 * c.n_kv_heads);
     if (n > c.T / 1024) n = c.T / 1024;
     if (n > KV_TOKENS) n = KV_TOKENS;
     return n < 1 ? 1 : static_cast<int>(n);
@@ -275,7 +277,7 @@ int tokens_of(const KvCacheArgs& c) {
 
 hipError_t launch_kv_write(const KvCacheArgs& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                            int act_dtype, const float* m_in, hipStream_t stream) {
-    const int n = tokens_of(c);
+    const int n = tokens_of(c, 16);
     kv_dispatch(c, act_dtype == 1, [&](auto dh, auto e4m3, auto bf16) {
         hipLaunchKernelGGL((kv_write_kernel<decltype(dh)::value, decltype(e4m3)::value, decltype(bf16)::value>),
                            dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n, k, k_stride,
@@ -285,7 +287,7 @@ hipError_t launch_kv_write(const KvCacheArgs& c, const void* k, int64_t k_stride
 }
 
 hipError_t launch_kv_read(const KvCacheArgs& c, void* k, void* v, int out_dtype, float* m, hipStream_t stream) {
-    const int n = tokens_of(c);
+    const int n = tokens_of(c, 4);
     kv_dispatch(c, out_dtype == 1, [&](auto dh, auto e4m3, auto bf16) {
         hipLaunchKernelGGL((kv_read_kernel<decltype(dh)::value, decltype(e4m3)::value, decltype(bf16)::value>),
                            dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n, k, v, m);
