@@ -28,9 +28,12 @@ namespace {
 constexpr int DE_THREADS = 256;
 constexpr int DE_WAVES = DE_THREADS / kWave;
 constexpr int DE_ROWS = 16;        // query heads of a group that are worked on together
-// Workgroups per CU and in all.
-__host__ __device__ constexpr int per_cu(bool e4m3) { return e4m3 ? 3 : 2; }
-__host__ __device__ constexpr int workers(bool e4m3) { return 256 * per_cu(e4m3); }
+// Workgroups per CU, as many as fit with their registers, and in all. A wave has about a tile of keys and
+// values in flight, 16 KB with rows of 256 bytes, 8 with 128, 4 with 64: the smaller the rows, the more waves it
+// takes. us with two / three / four a CU: 131072 keys of bf16 x 128 90 / 93 / -, 64 sequences of e4m3 x 128
+// 115 / 110 / 171 (spills), of e4m3 x 64 96 / 79 / 72, of bf16 x 64 - / 106 / 107.
+__host__ __device__ constexpr int per_cu(int dh, bool e4m3) { return (dh == 128 ? 2 : 3) + (e4m3 ? 1 : 0); }
+__host__ __device__ constexpr int workers(int dh, bool e4m3) { return 256 * per_cu(dh, e4m3); }
 constexpr float DE_LAZY = 8.f;     // the reference maximum moves when it is passed by this (log2)
 
 // Layout of the workspace: 2 partial results per worker, then the plan that the join reads: the
@@ -119,6 +122,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p, int bytes)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, kBufferFlags);
 }
 
+// Lanes whose bit D is clear get a[l] + a[l ^ D], the others b[l] + b[l ^ D].
+template <int D>
+__device__ __forceinline__ float sum_halves(float a, float b) {
+    if constexpr (D == 32) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    } else {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+}
+
 // The maximum of lanes l, l ^ 16, l ^ 32 and l ^ 48 (swaps of registers' rows: no trip through LDS).
 __device__ __forceinline__ float max_over_groups(float x) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -135,15 +150,14 @@ __device__ __forceinline__ f32x4_t product(float a, float b, f32x4_t acc) {
 }
 
 template <int DH, bool E4M3, int NS, int QR>
-__global__ void __launch_bounds__(DE_THREADS) __attribute__((amdgpu_waves_per_eu(per_cu(E4M3), DH == 128 ? per_cu(E4M3) : 4)))
+__global__ void __launch_bounds__(DE_THREADS) __attribute__((amdgpu_waves_per_eu(per_cu(DH, E4M3), per_cu(DH, E4M3))))
 decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __restrict__ block_table,
               const int32_t* __restrict__ seq_lens, float* __restrict__ part, int64_t* __restrict__ plan) {
     using T = DecodeTile<DH, E4M3, NS>;
     constexpr int NQ = DH / 32;  // 32-wide slices of the logits' contraction
     constexpr int PITCH = DH + 4;
-    constexpr int NP = DE_WAVES * 16 / QR;  // partial results of a run: per wave, with QR = 4 per wave and 16 lanes
-    __shared__ __attribute__((aligned(16))) float acc_s[NP][QR][PITCH];
-    __shared__ float max_s[DE_WAVES][QR];
+    // results of a run, per wave; with QR = 4 of two runs in turn, which saves a barrier
+    __shared__ __attribute__((aligned(16))) float res_s[QR == 4 ? 2 : 1][DE_WAVES][QR][PITCH];
     __shared__ int64_t scan_s[DE_WAVES];
     __shared__ int64_t in_seq_s;
     __shared__ int found_s[2];
@@ -154,7 +168,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     const int w = static_cast<int>(blockIdx.x);
 
     // ---- zeros for the sequences without a token
-    for (int b = w; b < a.n_seq; b += workers(E4M3)) {
+    for (int b = w; b < a.n_seq; b += workers(DH, E4M3)) {
         if (seq_lens[b] > 0) continue;
         for (int x = threadIdx.x; x < a.H * (DH / 4); x += DE_THREADS)
             store_row4(a, static_cast<int64_t>(b) * a.H + x / (DH / 4), DH, x % (DH / 4) * 4, f32x4_t{}, f32x4_t{});
@@ -197,7 +211,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
     total *= HR;
     if (w == 0 && threadIdx.x == 0) plan[0] = total;
-    const Share share(total, workers(E4M3));
+    const Share share(total, workers(DH, E4M3));
     int64_t g = share.start(w);
     const int64_t g_end = share.start(w + 1);
     if (g == g_end) return;
@@ -325,6 +339,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     load_v_m();
     fetch();
     bool first = true;
+    int parity = 0;
 
     // ---- runs of tiles
     while (true) {
@@ -428,58 +443,71 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             load_v_m();
         }
 
-        // ---- the four waves' results of this run: common maximum, then sums through LDS
-        __syncthreads();  // the last run's are read
-        if (lane < QR) max_s[wave][lane] = m_run;
-        __syncthreads();
-        float mt = max_s[0][lq];
+        // ---- the four waves' results of this run through LDS: unscaled sums and maximum of each
+        if constexpr (QR == 16) __syncthreads();  // the last run's are read
+        float(&res)[DE_WAVES][QR][PITCH] = res_s[QR == 4 ? parity : 0];
+        parity ^= 1;
+        float* dst = res[wave][lq];
+        if constexpr (QR == 16) {  // element e of acc[n]: dim (4 g4 + e) VN + n of query l % 16
 #pragma unroll
-        for (int i = 1; i < DE_WAVES; ++i) mt = fmaxf(mt, max_s[i][lq]);
-        const float wt = __builtin_amdgcn_exp2f(m_run - (mt == -INFINITY ? 0.f : mt));
-        // element e of acc[n]: dim (4 c + e) VN + n of query l % QR, c = l / 16 (QR = 16) or l % 16 / 4
-        const int c4 = QR == 16 ? g4 : l16 >> 2;
-        float* dst = acc_s[QR == 16 ? wave : wave * 4 + g4][lq];
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+                for (int n = 0; n < T::VN; n += 4)
+                    *reinterpret_cast<f32x4_t*>(dst + (4 * g4 + e) * T::VN + n) =
+                        f32x4_t{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]};
+        } else {
+            // Element e of acc[n]: this 16 lanes' part of dim (4 c + e) VN + n of query l % 4, c = l % 16 / 4. Two
+            // elements at a time are summed over half of the lanes each, so that a lane ends up with
+            // e = 2 (g4 % 2) + g4 / 2.
+            float sum[T::VN];
+#pragma unroll
+            for (int n = 0; n < T::VN; ++n) {
+                const float lo = sum_halves<32>(acc[n][0], acc[n][1]), hi = sum_halves<32>(acc[n][2], acc[n][3]);
+                sum[n] = sum_halves<16>(lo, hi);
+            }
+            const int e = 2 * (g4 & 1) + (g4 >> 1);
 #pragma unroll
             for (int n = 0; n < T::VN; n += 4)
-                *reinterpret_cast<f32x4_t*>(dst + (4 * c4 + e) * T::VN + n) =
-                    f32x4_t{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]} * wt;
-        if (c4 == 0)  // vision, text, sum (-1: no key seen), maximum
-            *reinterpret_cast<f32x4_t*>(dst + DH) =
-                f32x4_t{acc[T::VN][0] * wt, acc[T::VN][1] * wt, seen ? acc[T::VN][2] * wt : -1.f, mt};
+                *reinterpret_cast<f32x4_t*>(dst + (4 * (l16 >> 2) + e) * T::VN + n) =
+                    f32x4_t{sum[n], sum[n + 1], sum[n + 2], sum[n + 3]};
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const float x = sum_halves<32>(acc[T::VN][i], acc[T::VN][i]);
+                acc[T::VN][i] = sum_halves<16>(x, x);
+            }
+        }
+        if (lane < QR)  // vision, text, sum (-1: no key seen), maximum
+            *reinterpret_cast<f32x4_t*>(dst + DH) = f32x4_t{acc[T::VN][0], acc[T::VN][1], seen ? acc[T::VN][2] : -1.f, m_run};
         __syncthreads();
         const bool whole = i0 == 0 && i1 == at.nb;
         float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH);
         for (int x = threadIdx.x; x < rows * (DH / 4); x += DE_THREADS) {
             const int r = x / (DH / 4), d = x % (DH / 4) * 4;
-            f32x4_t sum = f32x4_t{};
-            float l = 0.f;
+            f32x4_t y[DE_WAVES];
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < DE_WAVES; ++i) {
+                y[i] = *reinterpret_cast<const f32x4_t*>(&res[i][r][DH]);
+                top = fmaxf(top, y[i][3]);
+            }
+            const float base = top == -INFINITY ? 0.f : top;
+            f32x4_t sum{}, st{};
             bool any = false;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                sum += *reinterpret_cast<const f32x4_t*>(&acc_s[i][r][d]);
-                const float li = acc_s[i][r][DH + 2];
-                any |= li != -1.f;
-                l += li != -1.f ? li : 0.f;
+            for (int i = 0; i < DE_WAVES; ++i) {
+                if (y[i][2] == -1.f) continue;  // saw no key: all zeros
+                const float wt = __builtin_amdgcn_exp2f(y[i][3] - base);
+                sum += *reinterpret_cast<const f32x4_t*>(&res[i][r][d]) * wt;
+                st += f32x4_t{y[i][0], y[i][1], y[i][2], 0.f} * wt;
+                any = true;
             }
             const int64_t head = static_cast<int64_t>(at.b) * a.H + hk * a.group + row0 + r;
-            f32x4_t st{};
-            if (d == 0) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    st[0] += acc_s[i][r][DH];
-                    st[1] += acc_s[i][r][DH + 1];
-                }
-                st[2] = any ? l : -1.f;
-                st[3] = acc_s[0][r][DH + 3];
-            }
             if (whole) {
-                const float inv = any ? 1.f / l : 0.f;  // nothing held: zeros
+                const float inv = any ? 1.f / st[2] : 0.f;  // nothing held: zeros
                 store_row4(a, head, DH, d, sum * inv, st * inv);
             } else {
                 *reinterpret_cast<f32x4_t*>(out + r * PITCH + d) = sum;
-                if (d == 0) *reinterpret_cast<f32x4_t*>(out + r * PITCH + DH) = st;
+                if (d == 0) *reinterpret_cast<f32x4_t*>(out + r * PITCH + DH) = f32x4_t{st[0], st[1], any ? st[2] : -1.f, top};
             }
         }
 
@@ -572,7 +600,7 @@ decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ se
 
 size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim, bool e4m3) {
     const int rows = H / n_kv_heads < DE_ROWS ? H / n_kv_heads : DE_ROWS;
-    return align_up(sizeof(float) * 2 * workers(e4m3) * partial_floats(rows, head_dim), 256) +
+    return align_up(sizeof(float) * 2 * workers(head_dim, e4m3) * partial_floats(rows, head_dim), 256) +
            sizeof(int64_t) * (1 + static_cast<size_t>(n_seq));
 }
 
@@ -597,7 +625,7 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
     a.m = c.m;
     a.o = static_cast<uint16_t*>(o);
     a.m_heads = m_heads;
-    const int W = workers(c.e4m3 != 0);
+    const int W = workers(c.head_dim, c.e4m3 != 0);
     float* part = static_cast<float*>(ws);
     int64_t* plan = reinterpret_cast<int64_t*>(
         static_cast<char*>(ws) + align_up(sizeof(float) * 2 * W * partial_floats(a.rows, c.head_dim), 256));
