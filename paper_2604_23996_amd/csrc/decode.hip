@@ -98,8 +98,8 @@ struct DecodeTile {
     static constexpr int TILE = DE_WAVES * 16 * NS;
     i32x4_t k[NS][KL];
     int v[NS][4][VB / 4];
-    i32x4_t m[NS];
-    int ks[NS], vs[NS];
+    i32x4_t m;           // lanes l % 4 = 0 and 1 of quads l / 4 % 4 = p: vision and text scores of piece p's keys 4 (l / 16) + 0..3
+    int scales;          // lane j = l % 16: four bytes, of the keys (j < 8) or values, piece j / 4 % 2, keys 4 (j % 4) ..
     int nk[NS], nv[NS];  // rows that are held, of the pieces in k and in v
 };
 
@@ -132,6 +132,11 @@ __device__ __forceinline__ float sum_halves(float a, float b) {
         const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
         return __uint_as_float(s[0]) + __uint_as_float(s[1]);
     }
+}
+
+// Byte e of four scale bytes as the power of two it stands for.
+__device__ __forceinline__ float scale_of(int x, int e) {
+    return __uint_as_float((e == 3 ? static_cast<uint32_t>(x) >> 1 : static_cast<uint32_t>(x) << (23 - 8 * e)) & 0x7f800000u);
 }
 
 // The maximum of lanes l, l ^ 16, l ^ 32 and l ^ 48 (swaps of registers' rows: no trip through LDS).
@@ -283,6 +288,12 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             mrow[s] = ((page * 2) << a.page_shift) + slot;
         }
     };
+    // The scales and scores of both pieces with one load each, every lane from its own address. (They
+    // cost what the number of loads is, not their bytes: 64 sequences in e4m3 110 us with a load per
+    // piece and array, 108 with these.) They lie inside a page, and page 0 stands for one that is not held.
+    static_assert(NS == 2, "a bit of the lane chooses the piece");
+    const uint8_t* scale_base = (l16 & 8 ? a.v_scale : a.k_scale) + 4 * (l16 & 3);
+    const float* m_base = a.m + ((lane & 1) << a.page_shift) + 4 * g4;
     // rows that are not held are outside their buffer: they read as zeros and cost nothing
     auto load_k = [&]() {
 #pragma unroll
@@ -293,9 +304,11 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                 const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, l16 * DH * T::ES + g4 * 16 + c * 64, 0, kBufferNonTemporal);
                 t.k[s][c] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
             }
-            if constexpr (E4M3)
-                t.ks[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.k_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, kBufferNonTemporal));
             t.nk[s] = held[s];
+        }
+        if constexpr (E4M3) {
+            const int64_t r0 = row[0], r1 = row[1];
+            t.scales = __builtin_nontemporal_load(reinterpret_cast<const int*>(scale_base + (l16 & 4 ? r1 : r0)));
         }
     };
     auto load_v_m = [&]() {
@@ -304,14 +317,10 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             const auto r = rsrc(a.v + row[s] * (DH * T::ES), held[s] * DH * T::ES);
 #pragma unroll
             for (int e = 0; e < 4; ++e) load_v<T::VB>(r, (g4 * 4 + e) * DH * T::ES + l16 * T::VB, t.v[s][e]);
-            if constexpr (E4M3)
-                t.vs[s] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rsrc(a.v_scale + row[s], (held[s] + 3) & ~3), g4 * 4, 0, kBufferNonTemporal));
-            // vision scores for lanes l % QR = 0, text for 1; the others read nothing
-            const auto rm = rsrc(a.m + mrow[s], a.m != nullptr && held[s] > 0 ? (4 << a.page_shift) + 64 : 0);
-            const auto x = __builtin_amdgcn_raw_buffer_load_b128(rm, lq < 2 ? (lq << (a.page_shift + 2)) + g4 * 16 : kOutOfRange, 0, kBufferNonTemporal);
-            t.m[s] = i32x4_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3])};
             t.nv[s] = held[s];
         }
+        const int64_t r0 = mrow[0], r1 = mrow[1];
+        t.m = __builtin_nontemporal_load(reinterpret_cast<const i32x4_t*>(m_base + (l16 & 4 ? r1 : r0)));
     };
 
     // Queries of `at`'s group as B fragments: slice c of lane l holds query l % QR, the dims of the key
@@ -328,7 +337,17 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         }
     };
 
-    const int one = lq == 2 ? 0x3f800000 : 0;  // the third row of the scores' product: 1.0
+    // The scores' product: quad p of 16 lanes works for piece p, its lanes' rows vision, text, 1 (the softmax
+    // denominator) and 0.
+    int score_mask[NS], one[NS];
+#pragma unroll
+    for (int p = 0; p < NS; ++p) {
+        score_mask[p] = l16 >> 2 == p && (lane & 3) < 2 ? -1 : 0;
+        one[p] = l16 >> 2 == p && (lane & 3) == 2 ? 0x3f800000 : 0;
+    }
+    auto scales_of = [&](int which, int p) {  // which: 0 keys, 1 values
+        return __builtin_amdgcn_ds_bpermute(4 * ((lane & 48) + 8 * which + 4 * p + g4), t.scales);
+    };
 
     fetch();
     load_q(at);
@@ -358,9 +377,15 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             // ---- logits, in units of log2
             f32x4_t s[NS];
             float mx = -INFINITY;
+            int vs[NS] = {};
 #pragma unroll
             for (int p = 0; p < NS; ++p) {
                 s[p] = f32x4_t{};
+                int ks = 0;
+                if constexpr (E4M3) {
+                    ks = scales_of(0, p);
+                    vs[p] = scales_of(1, p);
+                }
 #pragma unroll
                 for (int c = 0; c < NQ; ++c) {
                     bf16x8_t kf;
@@ -382,7 +407,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float x = s[p][e] * a.scale_log2;
-                    if constexpr (E4M3) x *= __uint_as_float((static_cast<uint32_t>(t.ks[p]) >> (8 * e) & 0xffu) << 23);
+                    if constexpr (E4M3) x *= scale_of(ks, e);
                     x = g4 * 4 + e < nk ? x : -INFINITY;
                     s[p][e] = x;
                     mx = fmaxf(mx, x);
@@ -418,8 +443,8 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                     const bool in = g4 * 4 + e < nv;
                     const float pr = __builtin_amdgcn_exp2f(s[p][e] - from);
                     float pv = pr;
-                    if constexpr (E4M3) pv = in ? pr * __uint_as_float((static_cast<uint32_t>(t.vs[p]) >> (8 * e) & 0xffu) << 23) : 0.f;
-                    const float mc = __int_as_float((t.m[p][e] & (in ? -1 : 0)) | one);
+                    if constexpr (E4M3) pv = in ? pr * scale_of(vs[p], e) : 0.f;
+                    const float mc = __int_as_float((t.m[e] & (in ? score_mask[p] : 0)) | one[p]);
 #pragma unroll
                     for (int n = 0; n < T::VN; n += 2) {
                         float v0, v1;
@@ -470,11 +495,18 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             for (int n = 0; n < T::VN; n += 4)
                 *reinterpret_cast<f32x4_t*>(dst + (4 * (l16 >> 2) + e) * T::VN + n) =
                     f32x4_t{sum[n], sum[n + 1], sum[n + 2], sum[n + 3]};
+        }
+        // The scores: QR = 4: element i of lane l is this quad's and 16 lanes' part; QR = 16: rows 0..3 (piece 0) are
+        // elements of lanes 0..15, rows 4..7 (piece 1) of lanes 16..31.
 #pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                const float x = sum_halves<32>(acc[T::VN][i], acc[T::VN][i]);
-                acc[T::VN][i] = sum_halves<16>(x, x);
+        for (int i = 0; i < 3; ++i) {
+            float x = acc[T::VN][i];
+            if constexpr (QR == 4) {
+                x = sum_halves<32>(x, x);
+                const int y = __float_as_int(x);  // the other quads of 16 lanes (two of the three are zero): row_ror 4 and 12
+                x += __int_as_float(dpp_mov<0x124>(y)) + __int_as_float(dpp_mov<0x12C>(y));
             }
+            acc[T::VN][i] = sum_halves<16>(x, x);
         }
         if (lane < QR)  // vision, text, sum (-1: no key seen), maximum
             *reinterpret_cast<f32x4_t*>(dst + DH) = f32x4_t{acc[T::VN][0], acc[T::VN][1], seen ? acc[T::VN][2] : -1.f, m_run};
@@ -622,7 +654,7 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
     a.v = static_cast<const uint8_t*>(c.v);
     a.k_scale = c.k_scale;
     a.v_scale = c.v_scale;
-    a.m = c.m;
+    a.m = c.m != nullptr ? c.m : static_cast<const float*>(c.k);  // read either way; the keys' pool is the larger one
     a.o = static_cast<uint16_t*>(o);
     a.m_heads = m_heads;
     const int W = workers(c.head_dim, c.e4m3 != 0);
