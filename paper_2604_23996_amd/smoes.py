@@ -404,12 +404,17 @@ def _gpu_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
     return dev
 
 
+# the handle of a GPU's current stream, without the Stream object where torch offers that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _launch(dev: int, where: str, fn, *args) -> None:
     if dev == torch.cuda.current_device():
-        status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+        status = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            status = fn(*args, _raw_stream(dev))
     if status != SMOES_OK:
         raise SmoesError(status, where)
 
@@ -418,33 +423,34 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _heads(t: torch.Tensor, name: str, dtype, shape) -> int:
-    """Checks a [tokens, heads, head_dim] tensor whose rows are dense inside a token; its token stride."""
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
+def _heads(t: torch.Tensor, name: str, dtype, n: int, h: int, d: int) -> int:
+    """Checks a [n tokens, h heads, d] tensor whose rows are dense inside a token; its token stride."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    n, h, d = shape
+    if t.shape != (n, h, d):
+        raise ValueError(f"{name}: expected {(n, h, d)}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return h * d
     s0, s1, s2 = t.stride()
-    if (s2 == 1 or d == 1) and (s1 == d or h == 1) and (s0 >= h * d or n == 1) or n * h * d == 0:
+    if (s2 == 1 or d == 1) and (s1 == d or h == 1) and (s0 >= h * d or n == 1):
         return s0 if n > 1 else h * d
     raise ValueError(f"{name}: the heads of a token have to be dense (strides {t.stride()})")
 
 
 def _array(t: Optional[torch.Tensor], name: str, dtype, shape) -> None:
-    if t is None:
+    if t is None or (t.dtype is dtype and t.shape == shape and t.is_contiguous()):
         return
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a dense {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name}: expected a dense {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def _sizes(t: torch.Tensor, name: str, head_dim: int):
     """Tokens and heads of a [tokens, heads, head_dim] tensor."""
-    if t.dim() != 3 or t.shape[2] != head_dim:
-        raise ValueError(f"{name}: expected [tokens, heads, {head_dim}], got {tuple(t.shape)}")
-    return t.shape[0], t.shape[1]
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != head_dim:
+        raise ValueError(f"{name}: expected [tokens, heads, {head_dim}], got {tuple(shape)}")
+    return shape[0], shape[1]
 
 
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -499,17 +505,17 @@ def rotary(plan: RotaryPlan, q: torch.Tensor, k: Optional[torch.Tensor] = None,
     Outputs are new dense tensors unless given (an input itself: in place). Returns (q_out, k_out or None)."""
     dt, dtype, dh = _dtype_code(q), q.dtype, plan.spec.head_dim
     T, H = _sizes(q, "q", dh)
-    q_stride = _heads(q, "q", dtype, q.shape)
+    q_stride = _heads(q, "q", dtype, T, H, dh)
     if q_out is None:
         q_out = torch.empty((T, H, dh), dtype=dtype, device=q.device)
-    qo_stride = _heads(q_out, "q_out", dtype, q.shape)
+    qo_stride = _heads(q_out, "q_out", dtype, T, H, dh)
     Hkv = k_stride = ko_stride = 0
     if k is not None:
         Hkv = _sizes(k, "k", dh)[1]
-        k_stride = _heads(k, "k", dtype, (T, Hkv, dh))
+        k_stride = _heads(k, "k", dtype, T, Hkv, dh)
         if k_out is None:
             k_out = torch.empty((T, Hkv, dh), dtype=dtype, device=q.device)
-        ko_stride = _heads(k_out, "k_out", dtype, k.shape)
+        ko_stride = _heads(k_out, "k_out", dtype, T, Hkv, dh)
     elif k_out is not None:
         raise ValueError("k_out without k")
     _array(positions, "positions", torch.int32, (T,))
@@ -576,9 +582,8 @@ def kv_write(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor, 
     """smoes_kv_write: append rows k, v [T, Hkv, head_dim] (bf16 or float32) and scores m_in [T, 2] behind what
     the sequences hold; seq_lens are the lengths with them. sample_offsets None: one token per sequence."""
     n_seq, max_pages = _kv_tables(block_table, seq_lens, sample_offsets)
-    T = k.shape[0]
-    shape = (T, cache.n_kv_heads, cache.head_dim)
-    k_stride, v_stride = _heads(k, "k", k.dtype, shape), _heads(v, "v", k.dtype, shape)
+    T, H, dh, dtype = k.shape[0], cache.n_kv_heads, cache.head_dim, k.dtype
+    k_stride, v_stride = _heads(k, "k", dtype, T, H, dh), _heads(v, "v", dtype, T, H, dh)
     _array(m_in, "m_in", torch.float32, (T, 2))
     dev = _gpu_of(cache.k, block_table, seq_lens, k, v, m_in, sample_offsets)
     _launch(dev, "smoes_kv_write", lib().smoes_kv_write, cache.desc, block_table.data_ptr(), max_pages,
@@ -626,7 +631,7 @@ def attention_scores_decode(cache: KVCache, block_table: torch.Tensor, seq_lens:
     n_seq, max_pages = _kv_tables(block_table, seq_lens, None)
     H = _sizes(q, "q", cache.head_dim)[1]
     shape = (n_seq, H, cache.head_dim)
-    q_stride = _heads(q, "q", torch.bfloat16, shape)
+    q_stride = _heads(q, "q", torch.bfloat16, *shape)
     if o is None:
         o = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
     if m_heads is None and cache.m is not None:
