@@ -709,7 +709,7 @@ int smoes_rotary_frequencies(const smoes_rotary* desc, double* freqs, float* amp
  *            An output may be its own input (same pointer and stride); any other
  *            overlap is not allowed.
  * desc's frequencies' fields are not read here, only head_dim, rot_dim and layout.
- * SMOES_ERR_SHAPE for T >= 2^31 or a token stride below the row (T > 1).
+ * SMOES_ERR_SHAPE for T >= 2^24 or a token stride below the row (T > 1).
  * Asynchronous on `stream`; nothing is allocated.
  */
 int smoes_rotary_apply(const smoes_rotary* desc, const double* freqs, float amplitude, const int32_t* positions,
@@ -765,6 +765,7 @@ typedef struct smoes_kv_cache {
  * m_in       [T, 2] float32 scores; required iff cache->m is not NULL.
  * A token whose position is negative, at or behind max_pages * page_size, or on a
  * page that is not held is not written. No two tokens of a call may have one place.
+ * SMOES_ERR_SHAPE for T >= 2^24, or T != n_seq without sample_offsets.
  * Asynchronous on `stream`; nothing is allocated.
  */
 int smoes_kv_write(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,
@@ -796,15 +797,15 @@ size_t smoes_attention_decode_workspace_size(const smoes_kv_cache* cache, int n_
  *   m_heads[b][h] = sum_j Attn_h(b, j) m[j]           (float32, 2 columns)
  * with Attn_h(b, .) = softmax over the held positions j of scale * q[b][h] . k[j][h_kv]
  * and h_kv = h / (n_heads / n_kv_heads). A sequence of which nothing is held (length 0, no
- * page) gets zeros. Positions at or behind the length are not read, whatever their pages hold.
- * q          [n_seq, n_heads, head_dim] bf16, q_stride elements from sequence to sequence.
+ * page) gets zeros. What the pages hold at or behind the length does not enter, NaN or not.
+ * q          [n_seq, n_heads, head_dim] bf16, q_stride elements from sequence to sequence. o must not overlap it.
  * scale      logit scale; <= 0 selects 1 / sqrt(head_dim).
  * o          [n_seq, n_heads, head_dim] bf16 output.
  * m_heads    [n_seq, n_heads, 2] float32 output, as smoes_attn_score_update takes it;
  *            required iff cache->m is not NULL.
  * The cached rows enter as they are read back; products and sums are float32.
  * The split of the work follows from all sequences' lengths: the same call gives
- * the same bits. n_heads % n_kv_heads == 0, n_heads <= 65535. Asynchronous on `stream`;
+ * the same bits. n_heads % n_kv_heads == 0, n_seq * n_heads < 2^24. Asynchronous on `stream`;
  * nothing is allocated; the workspace needs no initialisation.
  */
 int smoes_attention_scores_decode(const smoes_kv_cache* cache, const int32_t* block_table, int64_t max_pages,

@@ -50,6 +50,10 @@ int check_mi_shape(int64_t T, int E, int n_batch, int n_bins) {
     return SMOES_OK;
 }
 
+// A launch has at most a workgroup of 256 threads per token, or per sequence and head; a
+// launch's threads have to stay below 2^32.
+constexpr int64_t kTokensMax = (int64_t(1) << 24) - 1;
+
 static_assert(SMOES_HEAD_DIM_MAX == SMOES_HEAD_DIM_MAX_DEV, "the rotary kernels' LDS holds the largest head");
 
 int check_rotary(const smoes_rotary* r) {
@@ -81,9 +85,8 @@ int check_kv(const smoes_kv_cache* c, int64_t max_pages, int n_seq, KvCacheArgs*
     out->m = c->m;
     return SMOES_OK;
 }
-int check_kv_tokens(int64_t T, const smoes_kv_cache* c, int n_seq, const int32_t* sample_offsets) {
-    // token indexes are int32, and a workgroup takes at least one row of a token and head
-    if (T < 0 || T > INT32_MAX / 2 / c->n_kv_heads) return SMOES_ERR_SHAPE;
+int check_kv_tokens(int64_t T, int n_seq, const int32_t* sample_offsets) {
+    if (T < 0 || T > kTokensMax) return SMOES_ERR_SHAPE;
     if (sample_offsets == nullptr && T != n_seq) return SMOES_ERR_SHAPE;
     return SMOES_OK;
 }
@@ -334,7 +337,7 @@ int smoes_rotary_apply(const smoes_rotary* r, const double* freqs, float amplitu
     const int st = check_rotary(r);
     if (st != SMOES_OK) return st;
     if (amplitude != amplitude || (backward != 0 && backward != 1)) return SMOES_ERR_ARG;
-    if (T < 0 || T > INT32_MAX || n_heads < 1 || n_heads > 65535 || n_kv_heads < 0 || n_kv_heads > 65535)
+    if (T < 0 || T > kTokensMax || n_heads < 1 || n_heads > 65535 || n_kv_heads < 0 || n_kv_heads > 65535)
         return SMOES_ERR_SHAPE;
     const int64_t q_row = static_cast<int64_t>(n_heads) * r->head_dim, k_row = static_cast<int64_t>(n_kv_heads) * r->head_dim;
     if (T > 1 && (q_stride < q_row || q_out_stride < q_row)) return SMOES_ERR_SHAPE;
@@ -375,7 +378,7 @@ int smoes_kv_write(const smoes_kv_cache* cache, const int32_t* block_table, int6
     KvCacheArgs c;
     if (!dtype_ok(act_dtype)) return SMOES_ERR_ARG;
     int st = check_kv(cache, max_pages, n_seq, &c);
-    if (st == SMOES_OK) st = check_kv_tokens(T, cache, n_seq, sample_offsets);
+    if (st == SMOES_OK) st = check_kv_tokens(T, n_seq, sample_offsets);
     if (st != SMOES_OK) return st;
     const int64_t row = static_cast<int64_t>(cache->n_kv_heads) * cache->head_dim;
     if (T > 1 && (k_stride < row || v_stride < row)) return SMOES_ERR_SHAPE;
@@ -396,7 +399,7 @@ int smoes_kv_read(const smoes_kv_cache* cache, const int32_t* block_table, int64
     KvCacheArgs c;
     if (!dtype_ok(act_dtype)) return SMOES_ERR_ARG;
     int st = check_kv(cache, max_pages, n_seq, &c);
-    if (st == SMOES_OK) st = check_kv_tokens(T, cache, n_seq, sample_offsets);
+    if (st == SMOES_OK) st = check_kv_tokens(T, n_seq, sample_offsets);
     if (st != SMOES_OK) return st;
     if (T == 0 || n_seq == 0) return SMOES_OK;
     if ((st = check_kv_arrays(cache)) != SMOES_OK) return st;
@@ -425,13 +428,13 @@ int smoes_attention_scores_decode(const smoes_kv_cache* cache, const int32_t* bl
     int st = check_kv(cache, max_pages, n_seq, &c);
     if (st != SMOES_OK) return st;
     if (n_heads < 1 || n_heads > 65535 || (n_heads % cache->n_kv_heads) != 0) return SMOES_ERR_SHAPE;
-    if (static_cast<int64_t>(n_seq) * n_heads > INT32_MAX) return SMOES_ERR_SHAPE;
+    if (static_cast<int64_t>(n_seq) * n_heads > kTokensMax) return SMOES_ERR_SHAPE;
     if (n_seq > 1 && q_stride < static_cast<int64_t>(n_heads) * cache->head_dim) return SMOES_ERR_SHAPE;
     if (scale != scale) return SMOES_ERR_ARG;
     if (n_seq == 0) return SMOES_OK;
     if ((st = check_kv_arrays(cache)) != SMOES_OK) return st;
     if (block_table == nullptr || seq_lens == nullptr || q == nullptr || o == nullptr ||
-        (m_heads != nullptr) != (cache->m != nullptr))
+        (m_heads != nullptr) != (cache->m != nullptr) || o == q)
         return SMOES_ERR_ARG;
     if (workspace == nullptr || workspace_bytes < smoes_attention_decode_workspace_size(cache, n_seq, n_heads))
         return SMOES_ERR_WORKSPACE;

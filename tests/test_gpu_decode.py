@@ -322,3 +322,51 @@ def test_generation_matches_the_whole_sample(kind):
     torch.cuda.synchronize()
     for o, r in zip(got_o, rows_of):
         assert np.all(np.abs(o - host(whole)[r]) <= 1e-2 + 2e-2 * np.abs(o))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dh,H,Hkv", [(64, 4, 2), (128, 16, 2), (64, 18, 1)])
+def test_more_tiles_than_workgroups(kind, dh, H, Hkv):
+    # every workgroup has several tiles, most of more than one (sequence, group)
+    say("decode many tiles", kind, dh, H, Hkv)
+    rng = np.random.default_rng(21)
+    lens = rng.integers(2000, 4100, 26).astype(np.int32)
+    lens[[3, 4, 25]] = 0, 1, 128
+    c, _, table = make(rng, lens, 32, Hkv, dh, kind)
+    poison(c, table, lens)
+    q = queries(rng, 26, H, dh)
+    check(c, table, lens, q, *run(c, table, lens, q))
+
+
+@pytest.mark.parametrize("n_seq", [255, 256, 257, 512, 513, 770])
+def test_sequences_around_the_blocks_of_the_count(n_seq):
+    say("decode sequences", n_seq)
+    rng = np.random.default_rng(n_seq)
+    lens = rng.integers(0, 200, n_seq).astype(np.int32)
+    lens[[0, -1]] = 0, 150
+    c, _, table = make(rng, lens, 16, 1, 64, "bf16")
+    q = queries(rng, n_seq, 2, 64)
+    check(c, table, lens, q, *run(c, table, lens, q))
+
+
+def test_two_streams_at_once():
+    # calls that overlap in time, each with its own workspace, against the same calls one after another
+    say("decode streams")
+    rng = np.random.default_rng(22)
+    calls = []
+    for i, lens in enumerate(([3000, 17], [900, 2500])):
+        lens = np.array(lens, np.int32)
+        c, _, table = make(rng, lens, 16, 2, 128, "bf16")
+        calls.append((to_device(c), t(table), t(lens), t(queries(rng, 2, 8, 128))))
+    want = [S.attention_scores_decode(*a) for a in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = [[], []]
+    for _ in range(5):
+        for i, (a, st) in enumerate(zip(calls, streams)):
+            with torch.cuda.stream(st):
+                got[i].append(S.attention_scores_decode(*a))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for o, m in g:
+            assert torch.equal(o, w[0]) and torch.equal(m, w[1])

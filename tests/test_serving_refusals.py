@@ -48,7 +48,7 @@ def test_rotary_frequencies():
 
 def test_rotary_apply():
     assert _apply(T=0, q=None, k=None, qo=None, ko=None, freqs=None) == OK
-    assert _apply(T=-1) == SHAPE and _apply(T=1 << 31) == SHAPE
+    assert _apply(T=-1) == SHAPE and _apply(T=1 << 24) == SHAPE and _apply(T=1 << 31) == SHAPE
     assert _apply(H=0) == SHAPE and _apply(Hkv=-1) == SHAPE and _apply(H=70000) == SHAPE
     assert _apply(qs=127) == SHAPE and _apply(qos=127) == SHAPE and _apply(ks=63) == SHAPE and _apply(kos=0) == SHAPE
     assert _apply(rot=_rot(rot_dim=7)) == SHAPE
@@ -77,7 +77,7 @@ def _read(cache=None, bt=FAKE, max_pages=3, lens=FAKE, n_seq=2, off=FAKE, T=5, k
                                  m, None)
 
 
-def _decode(cache=None, bt=FAKE, max_pages=3, lens=FAKE, n_seq=2, q=FAKE, qs=256, H=4, scale=0.0, o=FAKE, m=FAKE,
+def _decode(cache=None, bt=FAKE, max_pages=3, lens=FAKE, n_seq=2, q=ctypes.c_void_p(0x2000), qs=256, H=4, scale=0.0, o=FAKE, m=FAKE,
             ws=FAKE, n=1 << 40):
     return S.lib().smoes_attention_scores_decode(_cache() if cache is None else cache, bt, max_pages, lens, n_seq, q,
                                                  qs, H, scale, o, m, ws, n, None)
@@ -89,7 +89,7 @@ def test_cache_sizes(call):
                dict(page_size=0), dict(page_size=-16), dict(n_kv_heads=0), dict(head_dim=96), dict(head_dim=0)):
         assert call(cache=_cache(**kw)) == SHAPE, kw
     assert call(cache=_cache(kind=2)) == ARG and call(cache=_cache(kind=-1)) == ARG
-    assert call(max_pages=0) == SHAPE and call(max_pages=(1 << 31) // 16) == SHAPE and call(n_seq=-1) == SHAPE
+    assert call(max_pages=0) == SHAPE and call(max_pages=(1 << 30) // 16 + 1) == SHAPE and call(n_seq=-1) == SHAPE
     # arrays: present, aligned, scales only where the kind has them
     for kw in (dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None), dict(k=0x1008), dict(v=0x1002),
                dict(k_scale=0x1002), dict(m=0x1004)):
@@ -100,7 +100,7 @@ def test_cache_sizes(call):
 def test_write_and_read():
     for call in (_write, _read):
         assert call(T=0) == OK and call(n_seq=0, T=3) == OK
-        assert call(T=-1) == SHAPE and call(T=(1 << 31) // 4) == SHAPE
+        assert call(T=-1) == SHAPE and call(T=1 << 24) == SHAPE
         assert call(off=None, T=5) == SHAPE  # one token per sequence
         assert call(dt=2) == ARG
     assert _write(ks=127) == SHAPE and _write(vs=0) == SHAPE
@@ -114,7 +114,8 @@ def test_write_and_read():
 def test_decode():
     assert _decode(n_seq=0) == OK
     assert _decode(H=3) == SHAPE and _decode(H=0) == SHAPE and _decode(qs=255) == SHAPE
-    assert _decode(n_seq=1 << 20, H=1 << 15) == SHAPE
+    assert _decode(n_seq=1 << 20, H=16) == SHAPE  # 2^24 workgroups
+    assert _decode(o=FAKE, q=FAKE) == ARG  # in place
     assert _decode(scale=math.nan) == ARG and _decode(q=None) == ARG and _decode(o=None) == ARG
     assert _decode(m=None) == ARG and _decode(cache=_cache(m=None)) == ARG
     need = S.lib().smoes_attention_decode_workspace_size(_cache(), 2, 4)
