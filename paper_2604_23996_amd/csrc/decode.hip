@@ -27,13 +27,21 @@ namespace {
 
 constexpr int DE_THREADS = 256;
 constexpr int DE_WAVES = DE_THREADS / kWave;
-constexpr int DE_ROWS = 16;        // query heads of a group that are worked on together
 // Workgroups per CU, as many as fit with their registers, and in all. A wave has about a tile of keys and
 // values in flight, 16 KB with rows of 256 bytes, 8 with 128, 4 with 64: the smaller the rows, the more waves it
 // takes. us with two / three / four a CU: 131072 keys of bf16 x 128 90 / 93 / -, 64 sequences of e4m3 x 128
 // 115 / 110 / 171 (spills), of e4m3 x 64 96 / 79 / 72, of bf16 x 64 - / 106 / 107.
-__host__ __device__ constexpr int per_cu(int dh, bool e4m3) { return (dh == 128 ? 2 : 3) + (e4m3 ? 1 : 0); }
-__host__ __device__ constexpr int workers(int dh, bool e4m3) { return 256 * per_cu(dh, e4m3); }
+// (Two sets of 16 query heads, RT = 2, take the registers of a workgroup more.)
+__host__ __device__ constexpr int per_cu(int dh, bool e4m3, int rt) {
+    return (dh == 128 ? 2 : 3) + (e4m3 && rt == 1 ? 1 : 0);
+}
+__host__ __device__ constexpr int workers(int dh, bool e4m3, int rt) { return 256 * per_cu(dh, e4m3, rt); }
+// Query heads of a KV head that share a pass over its rows: sets of QR = 4 or 16, one or two of them.
+// Above 16 heads two sets halve the passes over the cache: 16 sequences of 2000 to 20000 in bf16, 40 heads over 2, 54.5
+// -> 44.6 us, 64 sequences, 17 over 1, 95 -> 68, 64 over 1, 181 -> 121; in e4m3, where the products bound it,
+// 43.1 -> 42.6. At most 4 heads take the 4 x 4 products, a quarter of the matrix time.
+__host__ __device__ constexpr int sets_of(int group) { return group > 16 ? 2 : 1; }
+__host__ __device__ constexpr int rows_of(int group) { return group <= 4 ? 4 : 16 * sets_of(group); }
 constexpr float DE_LAZY = 8.f;     // the reference maximum moves when it is passed by this (log2)
 
 // Layout of the workspace: 2 partial results per worker, then the plan that the join reads: the
@@ -42,7 +50,7 @@ __host__ __device__ constexpr int partial_floats(int rows, int dh) { return rows
 
 struct DecodeArgs {
     int64_t n_pages, max_pages, q_stride;
-    int page_shift, n_kv_heads, n_seq, H, group, rgroups, rows;  // rows: query heads per tile of 16
+    int page_shift, n_kv_heads, n_seq, H, group, rgroups, rows;  // rows: query heads of a pass
     float scale_log2;
     const uint8_t* k;
     const uint8_t* v;
@@ -154,8 +162,9 @@ __device__ __forceinline__ f32x4_t product(float a, float b, f32x4_t acc) {
     else return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, acc, 0, 0, 0);
 }
 
-template <int DH, bool E4M3, int NS, int QR>
-__global__ void __launch_bounds__(DE_THREADS) __attribute__((amdgpu_waves_per_eu(per_cu(DH, E4M3), per_cu(DH, E4M3))))
+template <int DH, bool E4M3, int NS, int QR, int RT>
+__global__ void __launch_bounds__(DE_THREADS)
+__attribute__((amdgpu_waves_per_eu(per_cu(DH, E4M3, RT), per_cu(DH, E4M3, RT))))
 decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __restrict__ block_table,
               const int32_t* __restrict__ seq_lens, float* __restrict__ part, int64_t* __restrict__ plan) {
     using T = DecodeTile<DH, E4M3, NS>;
@@ -173,7 +182,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     const int w = static_cast<int>(blockIdx.x);
 
     // ---- zeros for the sequences without a token
-    for (int b = w; b < a.n_seq; b += workers(DH, E4M3)) {
+    for (int b = w; b < a.n_seq; b += workers(DH, E4M3, RT)) {
         if (seq_lens[b] > 0) continue;
         for (int x = threadIdx.x; x < a.H * (DH / 4); x += DE_THREADS)
             store_row4(a, static_cast<int64_t>(b) * a.H + x / (DH / 4), DH, x % (DH / 4) * 4, f32x4_t{}, f32x4_t{});
@@ -216,7 +225,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
     total *= HR;
     if (w == 0 && threadIdx.x == 0) plan[0] = total;
-    const Share share(total, workers(DH, E4M3));
+    const Share share(total, workers(DH, E4M3, RT));
     int64_t g = share.start(w);
     const int64_t g_end = share.start(w + 1);
     if (g == g_end) return;
@@ -325,15 +334,19 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
 
     // Queries of `at`'s group as B fragments: slice c of lane l holds query l % QR, the dims of the key
     // fragment it meets.
-    bf16x8_t qf[NQ];
+    bf16x8_t qf[RT][NQ];
     auto load_q = [&](const Place& p) {
         typedef int i32x4_u __attribute__((ext_vector_type(4), aligned(2)));
-        const int row0 = (p.hr % a.rgroups) * QR, head = (p.hr / a.rgroups) * a.group + row0 + min(lq, a.group - row0 - 1);
-        const uint16_t* qr = q + p.b * a.q_stride + static_cast<int64_t>(head) * DH;
+        const int row0 = (p.hr % a.rgroups) * (QR * RT);
 #pragma unroll
-        for (int c = 0; c < NQ; ++c) {
-            const int d = E4M3 ? 64 * (c >> 1) + 16 * g4 + 8 * (c & 1) : 32 * c + 8 * g4;
-            qf[c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const i32x4_u*>(qr + d));
+        for (int rt = 0; rt < RT; ++rt) {
+            const int head = (p.hr / a.rgroups) * a.group + min(row0 + rt * QR + lq, a.group - 1);
+            const uint16_t* qr = q + p.b * a.q_stride + static_cast<int64_t>(head) * DH;
+#pragma unroll
+            for (int c = 0; c < NQ; ++c) {
+                const int d = E4M3 ? 64 * (c >> 1) + 16 * g4 + 8 * (c & 1) : 32 * c + 8 * g4;
+                qf[rt][c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const i32x4_u*>(qr + d));
+            }
         }
     };
 
@@ -363,24 +376,30 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     // ---- runs of tiles
     while (true) {
         const int i0 = at.i, i1 = static_cast<int>(min(static_cast<int64_t>(at.nb), i0 + (g_end - g)));
-        const int hk = at.hr / a.rgroups, row0 = (at.hr % a.rgroups) * QR;
-        const int rows = min(QR, a.group - row0);
+        const int hk = at.hr / a.rgroups, row0 = (at.hr % a.rgroups) * (QR * RT);
         const bool more = g + (i1 - i0) < g_end;
         Place then = at;
-        f32x4_t acc[T::VN + 1];
+        f32x4_t acc[RT][T::VN + 1];
+        float m_run[RT];
 #pragma unroll
-        for (int n = 0; n <= T::VN; ++n) acc[n] = f32x4_t{};
-        float m_run = -INFINITY;
+        for (int rt = 0; rt < RT; ++rt) {
+            m_run[rt] = -INFINITY;
+#pragma unroll
+            for (int n = 0; n <= T::VN; ++n) acc[rt][n] = f32x4_t{};
+        }
         bool seen = false;
 
         for (int i = i0; i < i1; ++i) {
             // ---- logits, in units of log2
-            f32x4_t s[NS];
-            float mx = -INFINITY;
+            f32x4_t s[RT][NS];
+            float mx[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) mx[rt] = -INFINITY;
             int vs[NS] = {};
 #pragma unroll
             for (int p = 0; p < NS; ++p) {
-                s[p] = f32x4_t{};
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt][p] = f32x4_t{};
                 int ks = 0;
                 if constexpr (E4M3) {
                     ks = scales_of(0, p);
@@ -401,17 +420,21 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                     } else {
                         kf = __builtin_bit_cast(bf16x8_t, t.k[p][c]);
                     }
-                    s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c], s[p], 0, 0, 0);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+                        s[rt][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][c], s[rt][p], 0, 0, 0);
                 }
                 const int nk = t.nk[p];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = s[p][e] * a.scale_log2;
-                    if constexpr (E4M3) x *= scale_of(ks, e);
-                    x = g4 * 4 + e < nk ? x : -INFINITY;
-                    s[p][e] = x;
-                    mx = fmaxf(mx, x);
-                }
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        float x = s[rt][p][e] * a.scale_log2;
+                        if constexpr (E4M3) x *= scale_of(ks, e);
+                        x = g4 * 4 + e < nk ? x : -INFINITY;
+                        s[rt][p][e] = x;
+                        mx[rt] = fmaxf(mx[rt], x);
+                    }
                 seen |= nk > 0;
             }
             if (i + 1 == i1 && more) {
@@ -423,17 +446,21 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             fetch();
             __builtin_amdgcn_sched_barrier(0);
             // ---- running maximum, moved lazily
-            mx = max_over_groups(mx);
-            const bool grow = mx > m_run + DE_LAZY;
-            if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-                const float m_new = grow ? mx : m_run;
-                const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
-                m_run = m_new;
+            float from[RT];
 #pragma unroll
-                for (int n = 0; n <= T::VN; ++n) acc[n] *= alpha;
+            for (int rt = 0; rt < RT; ++rt) {
+                mx[rt] = max_over_groups(mx[rt]);
+                const bool grow = mx[rt] > m_run[rt] + DE_LAZY;
+                if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+                    const float m_new = grow ? mx[rt] : m_run[rt];
+                    const float alpha = grow ? __builtin_amdgcn_exp2f(m_run[rt] - m_new) : 1.f;
+                    m_run[rt] = m_new;
+#pragma unroll
+                    for (int n = 0; n <= T::VN; ++n) acc[rt][n] *= alpha;
+                }
+                // as long as every logit is minus infinity, exponents are taken from 0: their sum stays 0
+                from[rt] = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
             }
-            // as long as every logit is minus infinity, exponents are taken from 0: their sum stays 0
-            const float from = m_run == -INFINITY ? 0.f : m_run;
             // ---- probabilities, values, scores
 #pragma unroll
             for (int p = 0; p < NS; ++p) {
@@ -441,9 +468,12 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const bool in = g4 * 4 + e < nv;
-                    const float pr = __builtin_amdgcn_exp2f(s[p][e] - from);
-                    float pv = pr;
-                    if constexpr (E4M3) pv = in ? pr * scale_of(vs[p], e) : 0.f;
+                    float pr[RT], pv[RT];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        pv[rt] = pr[rt] = __builtin_amdgcn_exp2f(s[rt][p][e] - from[rt]);
+                        if constexpr (E4M3) pv[rt] = in ? pr[rt] * scale_of(vs[p], e) : 0.f;
+                    }
                     const float mc = __int_as_float((t.m[e] & (in ? score_mask[p] : 0)) | one[p]);
 #pragma unroll
                     for (int n = 0; n < T::VN; n += 2) {
@@ -458,10 +488,14 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                             v0 = __uint_as_float(y << 16);
                             v1 = __uint_as_float(y & 0xffff0000u);
                         }
-                        acc[n] = product<QR>(v0, pv, acc[n]);
-                        acc[n + 1] = product<QR>(v1, pv, acc[n + 1]);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            acc[rt][n] = product<QR>(v0, pv[rt], acc[rt][n]);
+                            acc[rt][n + 1] = product<QR>(v1, pv[rt], acc[rt][n + 1]);
+                        }
                     }
-                    acc[T::VN] = product<QR>(mc, pr, acc[T::VN]);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) acc[rt][T::VN] = product<QR>(mc, pr[rt], acc[rt][T::VN]);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -469,77 +503,81 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         }
 
         // ---- the four waves' results of this run through LDS: unscaled sums and maximum of each
-        if constexpr (QR == 16) __syncthreads();  // the last run's are read
-        float(&res)[DE_WAVES][QR][PITCH] = res_s[QR == 4 ? parity : 0];
-        parity ^= 1;
-        float* dst = res[wave][lq];
-        if constexpr (QR == 16) {  // element e of acc[n]: dim (4 g4 + e) VN + n of query l % 16
+        const bool whole = i0 == 0 && i1 == at.nb;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+        for (int rt = 0; rt < RT; ++rt) {
+            const int set0 = row0 + rt * QR, rows = min(QR, a.group - set0);
+            if constexpr (QR == 16) __syncthreads();  // the last run's are read
+            float(&res)[DE_WAVES][QR][PITCH] = res_s[QR == 4 ? parity : 0];
+            parity ^= 1;
+            float* dst = res[wave][lq];
+            if constexpr (QR == 16) {  // element e of acc[..][n]: dim (4 g4 + e) VN + n of query l % 16
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int n = 0; n < T::VN; n += 4)
+                        *reinterpret_cast<f32x4_t*>(dst + (4 * g4 + e) * T::VN + n) =
+                            f32x4_t{acc[rt][n][e], acc[rt][n + 1][e], acc[rt][n + 2][e], acc[rt][n + 3][e]};
+            } else {
+                // Element e of acc[..][n]: this 16 lanes' part of dim (4 c + e) VN + n of query l % 4, c = l % 16 / 4. Two
+                // elements at a time are summed over half of the lanes each, so that a lane ends up with
+                // e = 2 (g4 % 2) + g4 / 2.
+                float sum[T::VN];
+#pragma unroll
+                for (int n = 0; n < T::VN; ++n) {
+                    const float lo = sum_halves<32>(acc[rt][n][0], acc[rt][n][1]), hi = sum_halves<32>(acc[rt][n][2], acc[rt][n][3]);
+                    sum[n] = sum_halves<16>(lo, hi);
+                }
+                const int e = 2 * (g4 & 1) + (g4 >> 1);
 #pragma unroll
                 for (int n = 0; n < T::VN; n += 4)
-                    *reinterpret_cast<f32x4_t*>(dst + (4 * g4 + e) * T::VN + n) =
-                        f32x4_t{acc[n][e], acc[n + 1][e], acc[n + 2][e], acc[n + 3][e]};
-        } else {
-            // Element e of acc[n]: this 16 lanes' part of dim (4 c + e) VN + n of query l % 4, c = l % 16 / 4. Two
-            // elements at a time are summed over half of the lanes each, so that a lane ends up with
-            // e = 2 (g4 % 2) + g4 / 2.
-            float sum[T::VN];
-#pragma unroll
-            for (int n = 0; n < T::VN; ++n) {
-                const float lo = sum_halves<32>(acc[n][0], acc[n][1]), hi = sum_halves<32>(acc[n][2], acc[n][3]);
-                sum[n] = sum_halves<16>(lo, hi);
+                    *reinterpret_cast<f32x4_t*>(dst + (4 * (l16 >> 2) + e) * T::VN + n) =
+                        f32x4_t{sum[n], sum[n + 1], sum[n + 2], sum[n + 3]};
             }
-            const int e = 2 * (g4 & 1) + (g4 >> 1);
+            // The scores: QR = 4: element i of lane l is this quad's and 16 lanes' part; QR = 16: rows 0..3 (piece 0) are
+            // elements of lanes 0..15, rows 4..7 (piece 1) of lanes 16..31.
 #pragma unroll
-            for (int n = 0; n < T::VN; n += 4)
-                *reinterpret_cast<f32x4_t*>(dst + (4 * (l16 >> 2) + e) * T::VN + n) =
-                    f32x4_t{sum[n], sum[n + 1], sum[n + 2], sum[n + 3]};
-        }
-        // The scores: QR = 4: element i of lane l is this quad's and 16 lanes' part; QR = 16: rows 0..3 (piece 0) are
-        // elements of lanes 0..15, rows 4..7 (piece 1) of lanes 16..31.
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            float x = acc[T::VN][i];
-            if constexpr (QR == 4) {
-                x = sum_halves<32>(x, x);
-                const int y = __float_as_int(x);  // the other quads of 16 lanes (two of the three are zero): row_ror 4 and 12
-                x += __int_as_float(dpp_mov<0x124>(y)) + __int_as_float(dpp_mov<0x12C>(y));
+            for (int i = 0; i < 3; ++i) {
+                float x = acc[rt][T::VN][i];
+                if constexpr (QR == 4) {
+                    x = sum_halves<32>(x, x);
+                    const int y = __float_as_int(x);  // the other quads of 16 lanes (two of the three are zero): row_ror 4 and 12
+                    x += __int_as_float(dpp_mov<0x124>(y)) + __int_as_float(dpp_mov<0x12C>(y));
+                }
+                acc[rt][T::VN][i] = sum_halves<16>(x, x);
             }
-            acc[T::VN][i] = sum_halves<16>(x, x);
-        }
-        if (lane < QR)  // vision, text, sum (-1: no key seen), maximum
-            *reinterpret_cast<f32x4_t*>(dst + DH) = f32x4_t{acc[T::VN][0], acc[T::VN][1], seen ? acc[T::VN][2] : -1.f, m_run};
-        __syncthreads();
-        const bool whole = i0 == 0 && i1 == at.nb;
-        float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH);
-        for (int x = threadIdx.x; x < rows * (DH / 4); x += DE_THREADS) {
-            const int r = x / (DH / 4), d = x % (DH / 4) * 4;
-            f32x4_t y[DE_WAVES];
-            float top = -INFINITY;
+            if (lane < QR)  // vision, text, sum (-1: no key seen), maximum
+                *reinterpret_cast<f32x4_t*>(dst + DH) = f32x4_t{acc[rt][T::VN][0], acc[rt][T::VN][1], seen ? acc[rt][T::VN][2] : -1.f, m_run[rt]};
+            __syncthreads();
+                float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH) + rt * QR * PITCH;
+            for (int x = threadIdx.x; x < rows * (DH / 4); x += DE_THREADS) {
+                const int r = x / (DH / 4), d = x % (DH / 4) * 4;
+                f32x4_t y[DE_WAVES];
+                float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < DE_WAVES; ++i) {
-                y[i] = *reinterpret_cast<const f32x4_t*>(&res[i][r][DH]);
-                top = fmaxf(top, y[i][3]);
-            }
-            const float base = top == -INFINITY ? 0.f : top;
-            f32x4_t sum{}, st{};
-            bool any = false;
+                for (int i = 0; i < DE_WAVES; ++i) {
+                    y[i] = *reinterpret_cast<const f32x4_t*>(&res[i][r][DH]);
+                    top = fmaxf(top, y[i][3]);
+                }
+                const float base = top == -INFINITY ? 0.f : top;
+                f32x4_t sum{}, st{};
+                bool any = false;
 #pragma unroll
-            for (int i = 0; i < DE_WAVES; ++i) {
-                if (y[i][2] == -1.f) continue;  // saw no key: all zeros
-                const float wt = __builtin_amdgcn_exp2f(y[i][3] - base);
-                sum += *reinterpret_cast<const f32x4_t*>(&res[i][r][d]) * wt;
-                st += f32x4_t{y[i][0], y[i][1], y[i][2], 0.f} * wt;
-                any = true;
-            }
-            const int64_t head = static_cast<int64_t>(at.b) * a.H + hk * a.group + row0 + r;
-            if (whole) {
-                const float inv = any ? 1.f / st[2] : 0.f;  // nothing held: zeros
-                store_row4(a, head, DH, d, sum * inv, st * inv);
-            } else {
-                *reinterpret_cast<f32x4_t*>(out + r * PITCH + d) = sum;
-                if (d == 0) *reinterpret_cast<f32x4_t*>(out + r * PITCH + DH) = f32x4_t{st[0], st[1], any ? st[2] : -1.f, top};
+                for (int i = 0; i < DE_WAVES; ++i) {
+                    if (y[i][2] == -1.f) continue;  // saw no key: all zeros
+                    const float wt = __builtin_amdgcn_exp2f(y[i][3] - base);
+                    sum += *reinterpret_cast<const f32x4_t*>(&res[i][r][d]) * wt;
+                    st += f32x4_t{y[i][0], y[i][1], y[i][2], 0.f} * wt;
+                    any = true;
+                }
+                const int64_t head = static_cast<int64_t>(at.b) * a.H + hk * a.group + set0 + r;
+                if (whole) {
+                    const float inv = any ? 1.f / st[2] : 0.f;  // nothing held: zeros
+                    store_row4(a, head, DH, d, sum * inv, st * inv);
+                } else {
+                    *reinterpret_cast<f32x4_t*>(out + r * PITCH + d) = sum;
+                    if (d == 0) *reinterpret_cast<f32x4_t*>(out + r * PITCH + DH) = f32x4_t{st[0], st[1], any ? st[2] : -1.f, top};
+                }
             }
         }
 
@@ -631,8 +669,8 @@ decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ se
 }  // namespace
 
 size_t decode_workspace_bytes(int n_seq, int H, int n_kv_heads, int head_dim, bool e4m3) {
-    const int rows = H / n_kv_heads < DE_ROWS ? H / n_kv_heads : DE_ROWS;
-    return align_up(sizeof(float) * 2 * workers(head_dim, e4m3) * partial_floats(rows, head_dim), 256) +
+    const int group = H / n_kv_heads, rows = group < rows_of(group) ? group : rows_of(group);
+    return align_up(sizeof(float) * 2 * workers(head_dim, e4m3, sets_of(group)) * partial_floats(rows, head_dim), 256) +
            sizeof(int64_t) * (1 + static_cast<size_t>(n_seq));
 }
 
@@ -647,8 +685,8 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
     a.n_seq = c.n_seq;
     a.H = H;
     a.group = H / c.n_kv_heads;
-    a.rgroups = static_cast<int>(ceil_div(a.group, DE_ROWS));
-    a.rows = a.group < DE_ROWS ? a.group : DE_ROWS;
+    a.rgroups = static_cast<int>(ceil_div(a.group, rows_of(a.group)));
+    a.rows = a.group < rows_of(a.group) ? a.group : rows_of(a.group);
     a.scale_log2 = scale * 1.4426950408889634f;
     a.k = static_cast<const uint8_t*>(c.k);
     a.v = static_cast<const uint8_t*>(c.v);
@@ -657,7 +695,7 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
     a.m = c.m != nullptr ? c.m : static_cast<const float*>(c.k);  // read either way; the keys' pool is the larger one
     a.o = static_cast<uint16_t*>(o);
     a.m_heads = m_heads;
-    const int W = workers(c.head_dim, c.e4m3 != 0);
+    const int W = workers(c.head_dim, c.e4m3 != 0, sets_of(a.group));
     float* part = static_cast<float*>(ws);
     int64_t* plan = reinterpret_cast<int64_t*>(
         static_cast<char*>(ws) + align_up(sizeof(float) * 2 * W * partial_floats(a.rows, c.head_dim), 256));
@@ -666,7 +704,8 @@ hipError_t launch_decode(const KvCacheArgs& c, const void* q, int64_t q_stride, 
         constexpr int D = decltype(dh)::value, NS = 2;
         constexpr bool E = decltype(e4m3)::value;
         tile = DecodeTile<D, E, NS>::TILE;
-        const auto kernel = a.group <= 4 ? decode_kernel<D, E, NS, 4> : decode_kernel<D, E, NS, 16>;
+        const auto kernel = a.group <= 4 ? decode_kernel<D, E, NS, 4, 1>
+                            : sets_of(a.group) == 1 ? decode_kernel<D, E, NS, 16, 1> : decode_kernel<D, E, NS, 16, 2>;
         hipLaunchKernelGGL(kernel, dim3(W), dim3(DE_THREADS), 0, stream, a, static_cast<const uint16_t*>(q),
                            c.block_table, c.seq_lens, part, plan);
     });

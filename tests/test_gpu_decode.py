@@ -73,7 +73,7 @@ LENS = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 256, 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("H,Hkv,page", [(4, 4, 16), (8, 2, 32), (6, 1, 256), (20, 1, 16), (40, 2, 64), (17, 1, 128)])
+@pytest.mark.parametrize("H,Hkv,page", [(4, 4, 16), (8, 2, 32), (6, 1, 256), (20, 1, 16), (40, 2, 64), (17, 1, 128), (33, 1, 16), (70, 1, 32)])
 def test_ragged(kind, dh, H, Hkv, page):
     # every length around the tiles, among them 0; stale NaN behind every end; groups over and under 16 heads
     say("decode ragged", kind, dh, H, Hkv, page)
