@@ -181,13 +181,6 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     const int HR = a.n_kv_heads * a.rgroups;
     const int w = static_cast<int>(blockIdx.x);
 
-    // ---- zeros for the sequences without a token
-    for (int b = w; b < a.n_seq; b += workers(DH, E4M3, RT)) {
-        if (seq_lens[b] > 0) continue;
-        for (int x = threadIdx.x; x < a.H * (DH / 4); x += DE_THREADS)
-            store_row4(a, static_cast<int64_t>(b) * a.H + x / (DH / 4), DH, x % (DH / 4) * 4, f32x4_t{}, f32x4_t{});
-    }
-
     // ---- the plan: all tiles, this workgroup's range, and where it starts
     // sum over 256 sequences at a time of their tiles: inclusive prefix of this thread's, and the whole
     auto scan = [&](int n, int64_t& incl) {
@@ -225,6 +218,13 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
     total *= HR;
     if (w == 0 && threadIdx.x == 0) plan[0] = total;
+    // ---- zeros for the sequences without a token
+    for (int b = w; b < a.n_seq; b += workers(DH, E4M3, RT)) {
+        if (seq_lens[b] > 0) continue;
+        for (int x = threadIdx.x; x < a.H * (DH / 4); x += DE_THREADS)
+            store_row4(a, static_cast<int64_t>(b) * a.H + x / (DH / 4), DH, x % (DH / 4) * 4, f32x4_t{}, f32x4_t{});
+    }
+
     const Share share(total, workers(DH, E4M3, RT));
     int64_t g = share.start(w);
     const int64_t g_end = share.start(w + 1);
