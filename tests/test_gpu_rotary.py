@@ -50,6 +50,13 @@ CASES = [  # T, H, Hkv, head_dim, rot_dim, layout, scaling, dtype
     (12, 7, 3, 96, 48, "interleaved", "linear", torch.bfloat16),
     (300, 40, 2, 128, 64, "half", "by_parts", torch.bfloat16),
     (2, 3, 2, 512, 16, "interleaved", "none", torch.bfloat16),
+    (1200, 3, 1, 128, 66, "half", "none", torch.bfloat16),      # a last piece that shares values with the one before
+    (1100, 2, 1, 128, 66, "interleaved", "linear", torch.float32),
+    (40, 2, 1, 20, 18, "half", "none", torch.bfloat16),         # halves and a rest shorter or little longer than a piece
+    (40, 2, 1, 20, 18, "interleaved", "none", torch.float32),
+    (11, 1, 1, 12, 12, "half", "none", torch.bfloat16),
+    (3, 2, 2, 7, 6, "half", "none", torch.float32),
+    (3, 2, 2, 31, 30, "interleaved", "none", torch.bfloat16),
 ]
 
 
