@@ -2,22 +2,31 @@
 // token that is generated): o = sum_j p_j v_j and m = sum_j p_j M_j over the sequence's cached
 // tokens, p = softmax(scale q . k_j), in one pass with a running maximum and sum.
 //
-// What bounds it is reading the cache once: 4 head_dim flops per key, value and query head, and at
-// most the 16 query heads of a group share a row. The work is cut evenly over a fixed number of
-// workgroups, whatever the sequences' lengths are: the tiles (DE_TILE keys of one sequence and
-// group) of all sequences stand in one row, and the workgroups take N / W of them
-// each, in order. Lengths are only known on the device, so every workgroup counts the tiles
-// itself. A run of tiles of one (sequence, group) that a workgroup holds whole is finished by it;
-// of one that is shared, every workgroup leaves its maximum, sums and unscaled output in the
-// workspace, and decode_join_kernel puts them together.
+// What bounds it is reading the cache once: 4 head_dim flops per key, value and query head, and the
+// query heads of a group share its rows. 128 sequences of 4169 tokens on average, 16 KV heads of 128 in
+// bf16 (4.4 GB), take 667 us, 6.6 TB/s; one of 131072, 32 heads over 8, 89 us (6.0); 64 of 200 to 20000 in
+// e4m3, 32 over 8, 108 us (5.1: smaller rows, so fewer bytes in flight, and the scales besides).
 //
-// Layout, per wave and 16 keys: S^T = K Q^T with v_mfma_f32_16x16x32_bf16, A = K rows straight from
-// memory, B = the group's queries: lane l gets the logits of keys 4 (l / 16) + 0..3 and query l % 16.
-// O^T += V^T P^T with v_mfma_f32_16x16x4f32: product r's four keys are 4 k + r, so that its B operand
-// is register r of S^T after the exponential as it stands, and its A operand is what a lane loads
-// of row 4 (l / 16) + r, columns (l % 16) head_dim / 16 ...: a wave's loads are whole rows. Nothing moves
-// between lanes, and probabilities stay float32. A ninth product carries the scores: rows vision,
-// text and 1 (the softmax denominator).
+// The work is cut evenly over a fixed number of workgroups, whatever the sequences' lengths are: the tiles
+// (128 keys of one sequence and group) of all sequences stand in one row, and the workgroups take the same
+// number each, in order. Lengths are only known on the device, so every workgroup counts the tiles itself. A
+// run of tiles of one (sequence, group) that a workgroup holds whole is finished by it; of one that is shared,
+// every workgroup leaves its maximum, sums and unscaled output in the workspace, and decode_join_kernel puts
+// them together. A tile's loads go out while the tile before is worked on, across runs too; the rows come
+// straight from memory into the products' operands, with streaming loads (131072 keys: 101 us without).
+//
+// Layout, per wave and 16 keys: S^T = K Q^T with v_mfma_f32_16x16x32_bf16, A = K rows, B = the group's queries:
+// lane l gets the logits of keys 4 (l / 16) + 0..3 and query l % 16. Of a value row 4 (l / 16) + e a lane
+// loads columns (l % 16) head_dim / 16 ...: a wave's loads are whole rows, and the logit registers are, after
+// the exponential, where the products with V want the probabilities: nothing moves between lanes.
+//   Groups of up to 4 heads (QR = 4): the query columns hold the heads four times over, and
+//   v_mfma_f32_4x4x1f32, which treats four lanes by themselves, multiplies a key's four column pieces by its
+//   four probabilities in float32: 8 cycles for a column of 16 lanes, a quarter of the 16 x 16 form's.
+//   Larger groups (QR = 16): v_mfma_f32_16x16x32_bf16 over the tile's 32 keys per column, the probabilities as
+//   three bf16 terms whose sum is the float32 value to 2^-23: 48 cycles per column for the 256 of the float32 form (64
+//   heads over 8 in e4m3, 64 sequences of 200 to 20000: 146 -> 120 us; 40 over 2 in bf16: 44 -> 36).
+// The scores are carried by one more 4 x 4 product per key, float32: vision, text and 1 (the softmax
+// denominator).
 #include "common.h"
 #include "kernels.h"
 
@@ -37,9 +46,8 @@ __host__ __device__ constexpr int per_cu(int dh, bool e4m3, int rt) {
 }
 __host__ __device__ constexpr int workers(int dh, bool e4m3, int rt) { return 256 * per_cu(dh, e4m3, rt); }
 // Query heads of a KV head that share a pass over its rows: sets of QR = 4 or 16, one or two of them.
-// Above 16 heads two sets halve the passes over the cache: 16 sequences of 2000 to 20000 in bf16, 40 heads over 2, 54.5
-// -> 44.6 us, 64 sequences, 17 over 1, 95 -> 68, 64 over 1, 181 -> 121; in e4m3, where the products bound it,
-// 43.1 -> 42.6. At most 4 heads take the 4 x 4 products, a quarter of the matrix time.
+// Above 16 heads two sets halve the passes over the cache: 16 sequences of 2000 to 20000 in bf16, 40 heads over 2,
+// 54.5 -> 44.6 us, 64 sequences, 17 over 1, 95 -> 68, 64 over 1, 181 -> 121.
 __host__ __device__ constexpr int sets_of(int group) { return group > 16 ? 2 : 1; }
 __host__ __device__ constexpr int rows_of(int group) { return group <= 4 ? 4 : 16 * sets_of(group); }
 constexpr float DE_LAZY = 8.f;     // the reference maximum moves when it is passed by this (log2)
@@ -155,11 +163,24 @@ __device__ __forceinline__ float max_over_groups(float x) {
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// acc += a b over one key per 16 lanes
-template <int QR>
-__device__ __forceinline__ f32x4_t product(float a, float b, f32x4_t acc) {
-    if constexpr (QR == 16) return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, acc, 0, 0, 0);
+// Two probabilities as bf16 pairs whose sum is x to 2^-23: hi and mid are cut below the value (of x (1 - 2^-8),
+// of the rest likewise), so that no term of a positive x is zero or negative and an infinite value stays infinite.
+struct Split {
+    uint32_t hi, mid, lo;
+};
+__device__ __forceinline__ Split split_pair(float x0, float x1) {
+    constexpr float c = 1.f - 0x1p-8f;
+    Split s;
+    auto cut = [&](float& a, float& b) {  // the upper halves of a c and b c; a and b become what is left
+        const uint32_t u = __float_as_uint(a * c), v = __float_as_uint(b * c);
+        a -= __uint_as_float(u & 0xffff0000u);
+        b -= __uint_as_float(v & 0xffff0000u);
+        return __builtin_amdgcn_perm(v, u, 0x07060302u);
+    };
+    s.hi = cut(x0, x1);
+    s.mid = cut(x0, x1);
+    s.lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x0, x1}, bf16x2_t));
+    return s;
 }
 
 template <int DH, bool E4M3, int NS, int QR, int RT>
@@ -350,13 +371,15 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         }
     };
 
-    // The scores' product: quad p of 16 lanes works for piece p, its lanes' rows vision, text, 1 (the softmax
-    // denominator) and 0.
+    // The scores' product treats four lanes by themselves: rows vision, text, 1 (the softmax denominator) and 0 of a
+    // key, columns the four lanes' queries. QR = 4: the quads of 16 lanes have the same queries, and quad p works for
+    // piece p. QR = 16: every quad works for both.
     int score_mask[NS], one[NS];
 #pragma unroll
     for (int p = 0; p < NS; ++p) {
-        score_mask[p] = l16 >> 2 == p && (lane & 3) < 2 ? -1 : 0;
-        one[p] = l16 >> 2 == p && (lane & 3) == 2 ? 0x3f800000 : 0;
+        const bool mine = QR == 16 || l16 >> 2 == p;
+        score_mask[p] = mine && (lane & 3) < 2 ? -1 : 0;
+        one[p] = mine && (lane & 3) == 2 ? 0x3f800000 : 0;
     }
     auto scales_of = [&](int which, int p) {  // which: 0 keys, 1 values
         return __builtin_amdgcn_ds_bpermute(4 * ((lane & 48) + 8 * which + 4 * p + g4), t.scales);
@@ -462,40 +485,84 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                 from[rt] = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
             }
             // ---- probabilities, values, scores
+            Split ps[QR == 16 ? RT : 1][NS][2];  // of keys 0 and 1, 2 and 3 of a piece
 #pragma unroll
             for (int p = 0; p < NS; ++p) {
                 const int nv = t.nv[p];
+                float pv[RT][4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const bool in = g4 * 4 + e < nv;
-                    float pr[RT], pv[RT];
+                    // the quads hold piece 0's and 1's scores in turn: the next quad has the other's (row_ror 4)
+                    const int m_own = t.m[e], m_next = QR == 16 ? dpp_mov<0x124>(m_own) : m_own;
+                    const int m = (l16 >> 2 & 1) == p ? m_own : m_next;
+                    const float mc = __int_as_float((m & (in ? score_mask[p] : 0)) | one[p]);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
-                        pv[rt] = pr[rt] = __builtin_amdgcn_exp2f(s[rt][p][e] - from[rt]);
-                        if constexpr (E4M3) pv[rt] = in ? pr[rt] * scale_of(vs[p], e) : 0.f;
+                        const float pr = __builtin_amdgcn_exp2f(s[rt][p][e] - from[rt]);
+                        pv[rt][e] = pr;
+                        if constexpr (E4M3) pv[rt][e] = in ? pr * scale_of(vs[p], e) : 0.f;
+                        acc[rt][T::VN] = __builtin_amdgcn_mfma_f32_4x4x1f32(mc, pr, acc[rt][T::VN], 0, 0, 0);
                     }
-                    const float mc = __int_as_float((t.m[e] & (in ? score_mask[p] : 0)) | one[p]);
+                    if constexpr (QR == 4) {
 #pragma unroll
-                    for (int n = 0; n < T::VN; n += 2) {
-                        float v0, v1;
-                        if constexpr (E4M3) {
-                            const auto y = (n & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8(t.v[p][e][n / 4], true)
-                                                   : __builtin_amdgcn_cvt_pk_f32_fp8(t.v[p][e][n / 4], false);
-                            v0 = y[0];
-                            v1 = y[1];
-                        } else {
-                            const uint32_t y = static_cast<uint32_t>(t.v[p][e][n / 2]);
-                            v0 = __uint_as_float(y << 16);
-                            v1 = __uint_as_float(y & 0xffff0000u);
+                        for (int n = 0; n < T::VN; n += 2) {
+                            float v0, v1;
+                            if constexpr (E4M3) {
+                                const auto y = (n & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8(t.v[p][e][n / 4], true)
+                                                       : __builtin_amdgcn_cvt_pk_f32_fp8(t.v[p][e][n / 4], false);
+                                v0 = y[0];
+                                v1 = y[1];
+                            } else {
+                                const uint32_t y = static_cast<uint32_t>(t.v[p][e][n / 2]);
+                                v0 = __uint_as_float(y << 16);
+                                v1 = __uint_as_float(y & 0xffff0000u);
+                            }
+                            acc[0][n] = __builtin_amdgcn_mfma_f32_4x4x1f32(v0, pv[0][e], acc[0][n], 0, 0, 0);
+                            acc[0][n + 1] = __builtin_amdgcn_mfma_f32_4x4x1f32(v1, pv[0][e], acc[0][n + 1], 0, 0, 0);
+                        }
+                    }
+                }
+                if constexpr (QR == 16) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        ps[rt][p][0] = split_pair(pv[rt][0], pv[rt][1]);
+                        ps[rt][p][1] = split_pair(pv[rt][2], pv[rt][3]);
+                    }
+                }
+            }
+            if constexpr (QR == 16) {
+                // one product over the tile's 32 keys per column and term; word 2 p + i: keys 2 i and 2 i + 1 of piece p
+#pragma unroll
+                for (int n = 0; n < T::VN; n += 2) {
+                    union { uint32_t w[NS * 2]; bf16x8_t v; } v0, v1;
+#pragma unroll
+                    for (int p = 0; p < NS; ++p)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            if constexpr (E4M3) {
+                                const uint32_t x = __builtin_amdgcn_perm(t.v[p][2 * i + 1][n / 4], t.v[p][2 * i][n / 4],
+                                                                         n & 2 ? 0x07030602u : 0x05010400u);
+                                v0.w[2 * p + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
+                                v1.w[2 * p + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true));
+                            } else {
+                                v0.w[2 * p + i] = __builtin_amdgcn_perm(t.v[p][2 * i + 1][n / 2], t.v[p][2 * i][n / 2], 0x05040100u);
+                                v1.w[2 * p + i] = __builtin_amdgcn_perm(t.v[p][2 * i + 1][n / 2], t.v[p][2 * i][n / 2], 0x07060302u);
+                            }
                         }
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) {
-                            acc[rt][n] = product<QR>(v0, pv[rt], acc[rt][n]);
-                            acc[rt][n + 1] = product<QR>(v1, pv[rt], acc[rt][n + 1]);
-                        }
-                    }
+                    for (int rt = 0; rt < RT; ++rt) {
+                        auto term = [&](uint32_t Split::*which) {
+                            union { uint32_t w[NS * 2]; bf16x8_t v; } b;
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) acc[rt][T::VN] = product<QR>(mc, pr[rt], acc[rt][T::VN]);
+                            for (int i = 0; i < NS * 2; ++i) b.w[i] = ps[rt][i / 2][i % 2].*which;
+                            acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0.v, b.v, acc[rt][n], 0, 0, 0);
+                            acc[rt][n + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1.v, b.v, acc[rt][n + 1], 0, 0, 0);
+                        };
+                        term(&Split::lo);
+                        term(&Split::mid);
+                        term(&Split::hi);
+                    }
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -534,14 +601,12 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                     *reinterpret_cast<f32x4_t*>(dst + (4 * (l16 >> 2) + e) * T::VN + n) =
                         f32x4_t{sum[n], sum[n + 1], sum[n + 2], sum[n + 3]};
             }
-            // The scores: QR = 4: element i of lane l is this quad's and 16 lanes' part; QR = 16: rows 0..3 (piece 0) are
-            // elements of lanes 0..15, rows 4..7 (piece 1) of lanes 16..31.
+            // The scores' sums of 16 lanes each, and with QR = 4 of the quads (two of the four are zero).
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
-                float x = acc[rt][T::VN][i];
+                float x = sum_halves<32>(acc[rt][T::VN][i], acc[rt][T::VN][i]);
                 if constexpr (QR == 4) {
-                    x = sum_halves<32>(x, x);
-                    const int y = __float_as_int(x);  // the other quads of 16 lanes (two of the three are zero): row_ror 4 and 12
+                    const int y = __float_as_int(x);  // row_ror 4 and 12
                     x += __int_as_float(dpp_mov<0x124>(y)) + __int_as_float(dpp_mov<0x12C>(y));
                 }
                 acc[rt][T::VN][i] = sum_halves<16>(x, x);
@@ -588,8 +653,9 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
     }
 }
 
-// One workgroup per (sequence, query head): the partial results of the workers that share its tiles. Thread (group, four dims), the groups taking the workers in turn, a running
-// maximum and sums each; then the groups' results through LDS.
+// One workgroup per (sequence, query head): the partial results of the workers that share its tiles. Thread
+// (group, four dims), the groups taking the workers in turn, a running maximum and sums each; then the groups'
+// results through LDS. Bound by its chain of loads (5 to 7 us).
 template <int DH>
 __global__ void __launch_bounds__(DE_THREADS)
 decode_join_kernel(DecodeArgs a, int tile, int W, const int32_t* __restrict__ seq_lens, const float* __restrict__ part,

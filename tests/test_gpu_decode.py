@@ -153,6 +153,28 @@ def test_rising_and_falling_logits():
     check(c, table, lens, q, *run(c, table, lens, q))
 
 
+@pytest.mark.parametrize("H", [16, 40])
+def test_infinities_and_nan_in_wide_groups(H):
+    # groups over four heads, whose probabilities enter as three bf16 terms: an infinite value stays infinite in its
+    # column for every head, a NaN value NaN, and the other columns, sequences and the scores do not see them
+    say("decode infinities, wide groups", H)
+    rng = np.random.default_rng(23)
+    lens = np.array([90, 90, 90], np.int32)
+    c, _, table = make(rng, lens, 16, 2, 64, "bf16")
+    q = queries(rng, 3, H, 64, std=0.2)
+    put = lambda b, j, d, bits: c["v"][table[b, j // 16], 0, j % 16].__setitem__(d, bits)
+    for j in (0, 33, 89):  # other tiles, pieces and lanes
+        put(0, j, 3, 0x7f80)
+        put(0, j, 4, 0xff80)
+    put(1, 40, 5, 0x7fc0)
+    o, mh = run(c, table, lens, q)
+    o, mh, g = host(o), host(mh), H // 2
+    assert (o[0, :g, 3] == np.inf).all() and (o[0, :g, 4] == -np.inf).all()
+    assert np.isfinite(np.delete(o[0, :g], [3, 4], axis=1)).all() and np.isfinite(o[0, g:]).all()
+    assert np.isnan(o[1, :g, 5]).all() and np.isfinite(np.delete(o[1, :g], 5, axis=1)).all()
+    assert np.isfinite(o[1, g:]).all() and np.isfinite(o[2]).all() and np.isfinite(mh).all()
+
+
 def test_infinities_and_nan():
     # a NaN or an infinity in a held row reaches its own sequence and heads, as in the formula, and no other
     say("decode infinities")
