@@ -709,7 +709,7 @@ int smoes_rotary_frequencies(const smoes_rotary* desc, double* freqs, float* amp
  *            An output may be its own input (same pointer and stride); any other
  *            overlap is not allowed.
  * desc's frequencies' fields are not read here, only head_dim, rot_dim and layout.
- * SMOES_ERR_SHAPE for T >= 2^24 or a token stride below the row (T > 1).
+ * SMOES_ERR_SHAPE for T >= 2^24, n_heads + n_kv_heads > 65535 or a token stride below the row (T > 1).
  * Asynchronous on `stream`; nothing is allocated.
  */
 int smoes_rotary_apply(const smoes_rotary* desc, const double* freqs, float amplitude, const int32_t* positions,

@@ -337,7 +337,7 @@ int smoes_rotary_apply(const smoes_rotary* r, const double* freqs, float amplitu
     const int st = check_rotary(r);
     if (st != SMOES_OK) return st;
     if (amplitude != amplitude || (backward != 0 && backward != 1)) return SMOES_ERR_ARG;
-    if (T < 0 || T > kTokensMax || n_heads < 1 || n_heads > 65535 || n_kv_heads < 0 || n_kv_heads > 65535)
+    if (T < 0 || T > kTokensMax || n_heads < 1 || n_kv_heads < 0 || n_heads > 65535 || n_kv_heads > 65535 - n_heads)
         return SMOES_ERR_SHAPE;
     const int64_t q_row = static_cast<int64_t>(n_heads) * r->head_dim, k_row = static_cast<int64_t>(n_kv_heads) * r->head_dim;
     if (T > 1 && (q_stride < q_row || q_out_stride < q_row)) return SMOES_ERR_SHAPE;

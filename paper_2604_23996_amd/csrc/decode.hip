@@ -72,8 +72,7 @@ struct DecodeArgs {
 // Four dims of a head's output, and with the first four its scores.
 __device__ __forceinline__ void store_row4(const DecodeArgs& a, int64_t head, int dh, int d, f32x4_t o, f32x4_t m) {
     *reinterpret_cast<uint2*>(a.o + head * dh + d) =
-        make_uint2(f32_to_bf16(o[0]) | static_cast<uint32_t>(f32_to_bf16(o[1])) << 16,
-                   f32_to_bf16(o[2]) | static_cast<uint32_t>(f32_to_bf16(o[3])) << 16);
+        make_uint2(cvt_bf16x2(o[0], o[1]), cvt_bf16x2(o[2], o[3]));
     if (d == 0 && a.m_heads != nullptr) {
         a.m_heads[2 * head] = m[0];
         a.m_heads[2 * head + 1] = m[1];
@@ -100,7 +99,6 @@ struct Share {
 
 __device__ __forceinline__ int seq_len(int len, int cap) { return min(max(len, 0), cap); }
 
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
 
@@ -179,7 +177,7 @@ __device__ __forceinline__ Split split_pair(float x0, float x1) {
     };
     s.hi = cut(x0, x1);
     s.mid = cut(x0, x1);
-    s.lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x0, x1}, bf16x2_t));
+    s.lo = cvt_bf16x2(x0, x1);
     return s;
 }
 

@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int
                 uint32_t w[N / 2];
 #pragma unroll
                 for (int e = 0; e < N; e += 2)
-                    w[e / 2] = f32_to_bf16(x[u][e]) | static_cast<uint32_t>(f32_to_bf16(x[u][e + 1])) << 16;
+                    w[e / 2] = cvt_bf16x2(x[u][e], x[u][e + 1]);
                 if (keep) store_words(static_cast<uint16_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
             }
         }
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
             if constexpr (OUT_BF16) {
                 uint32_t w[N / 2];
 #pragma unroll
-                for (int i = 0; i < N; i += 2) w[i / 2] = f32_to_bf16(e[i]) | static_cast<uint32_t>(f32_to_bf16(e[i + 1])) << 16;
+                for (int i = 0; i < N; i += 2) w[i / 2] = cvt_bf16x2(e[i], e[i + 1]);
                 store_words(static_cast<uint16_t*>(y) + at, w);
             } else {
 #pragma unroll

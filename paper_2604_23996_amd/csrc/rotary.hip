@@ -12,27 +12,35 @@ namespace {
 
 constexpr int RO_THREADS = 256;
 
-// cos and sin of position * freq radians (sin negated for the gradient).
-__device__ __forceinline__ float2 turn(int position, double freq, int backward) {
+// amplitude times cos and sin of position * freq radians (sin negated for the gradient).
+__device__ __forceinline__ float2 turn(int position, double freq, float amplitude, int backward) {
     const double turns = static_cast<double>(position) * freq * 0.15915494309189535;
     float s, c;
     sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &s, &c);
-    return make_float2(c, backward ? -s : s);
+    return make_float2(amplitude * c, backward ? -amplitude * s : amplitude * s);
 }
+
+// n / d by a multiplication: m = ceil(2^31 / d), exact for n d < 2^31.
+struct Divisor {
+    uint32_t d, m;
+    explicit Divisor(int64_t d) : d(static_cast<uint32_t>(d)), m(static_cast<uint32_t>(((int64_t(1) << 31) + d - 1) / d)) {}
+    __device__ int of(int n) const { return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(n)) * m >> 31); }
+};
 
 // A workgroup per `tokens` tokens: the sines and cosines of all of them into LDS, meanwhile the first
 // loads on their way. An item is a piece of a head: V consecutive values, 16 bytes, that hold pairs
 // (HALF: one piece of each half) or are copied. The last piece of either part is moved back to end with it:
 // values that it shares with the piece before are computed twice from the same input, and in place not stored
 // again. A part shorter than a piece goes value by value. Accesses are 16 bytes wide at any element, so that an
-// odd half (a rot_dim of 66: 8000 tokens of 32 + 8 heads of 128 take 39 us, with 64 35) or view needs no path of its own.
+// odd half (a rot_dim of 66: 8000 tokens of 32 + 8 heads of 128 take 35 us, with 64 33) or view needs no path of its own.
 //
 // Bound by reading and writing every value once: 16384 tokens of 32 + 8 heads of 128 in bf16 take
-// 63 us, 5.3 TB/s (a large copy runs at 5.05). Streaming stores bring 58.6 us here, but what reads the
-// rotated tensors next pays more for it: with the cache's write and the attention behind it 420
-// instead of 405 us at 16384 tokens, 105 instead of 98 at 4096. They stay ordinary stores.
+// 62 us, 5.4 TB/s (a large copy runs at 5.05); with divisions by the compiler and roundings in integer
+// arithmetic, whose instructions kept the vector ALUs busy, 65. Streaming stores brought 58.6 us for 63.6,
+// but what reads the rotated tensors next pays more for it: with the cache's write and the attention
+// behind it 420 instead of 405 us at 16384 tokens, 105 instead of 98 at 4096. They stay ordinary stores.
 template <bool BF16, bool HALF>
-__global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int tokens) {
+__global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int tokens, Divisor token, Divisor head) {
     constexpr int V = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;  // values of a piece, bytes of a value
     constexpr int PAIRS = HALF ? V : V / 2;             // pairs of an item
     typedef uint32_t piece __attribute__((ext_vector_type(4), aligned(2)));
@@ -41,8 +49,8 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
     const int half = a.rot_dim / 2, rest = a.head_dim - a.rot_dim;
     const int64_t t0 = static_cast<int64_t>(blockIdx.x) * tokens;
     const int nt = static_cast<int>(min(static_cast<int64_t>(tokens), a.T - t0));
-    const int pair_items = (half + PAIRS - 1) / PAIRS, per_head = pair_items + (rest + V - 1) / V;
-    const int heads = a.n_heads + a.n_kv_heads, per_token = heads * per_head, items = nt * per_token;
+    const int pair_items = (half + PAIRS - 1) / PAIRS;
+    const int per_head = static_cast<int>(head.d), per_token = static_cast<int>(token.d), items = nt * per_token;
     const bool no_short = (HALF ? half : a.rot_dim) >= V && (rest == 0 || rest >= V);  // every part holds a piece
     const int second = half * ES;  // bytes from a pair's first value to its second (HALF)
 
@@ -55,7 +63,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
     };
     auto item = [&](int it) {
         Item r;
-        const int t = it / per_token, j = it - t * per_token, h = j / per_head, i = j - h * per_head;
+        const int t = tokens == 1 ? 0 : token.of(it), j = it - t * per_token, h = head.of(j), i = j - h * per_head;
         const bool is_q = h < a.n_heads, pairs = i < pair_items;
         const int hh = is_q ? h : h - a.n_heads;
         const int part = pairs ? (HALF ? half : a.rot_dim) : rest, c = (pairs ? i : i - pair_items) * V;
@@ -88,7 +96,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
         if constexpr (BF16) reinterpret_cast<uint16_t*>(p)[e] = f32_to_bf16(v);
         else reinterpret_cast<float*>(p)[e] = v;
     };
-    constexpr int U = 2;  // items of a thread in flight (four, and 1024 a workgroup: 69.3 us for the 63 above)
+    constexpr int U = 2;  // items of a thread in flight (four, and 1024 a workgroup, took 69.3 us for 63.4)
     Item r[U];
     u32x4 p0[U], p1[U];
     auto load = [&](int base) {
@@ -106,7 +114,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
     for (int i = threadIdx.x; i < nt * half; i += RO_THREADS) {
         const int t = i / half;
         const int pos = a.positions != nullptr ? a.positions[t0 + t] : static_cast<int>(t0 + t);
-        cs[i] = turn(pos, a.freqs[i - t * half], a.backward);
+        cs[i] = turn(pos, a.freqs[i - t * half], a.amplitude, a.backward);
     }
     __syncthreads();
     auto get = [&](const u32x4& p, int e) {
@@ -114,7 +122,7 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
         else return __uint_as_float(p[e]);
     };
     auto put = [&](u32x4& p, int e, float v0, float v1) {  // values e and e + 1, e even
-        if constexpr (BF16) p[e / 2] = f32_to_bf16(v0) | static_cast<uint32_t>(f32_to_bf16(v1)) << 16;
+        if constexpr (BF16) p[e / 2] = cvt_bf16x2(v0, v1);
         else {
             p[e] = __float_as_uint(v0);
             p[e + 1] = __float_as_uint(v1);
@@ -135,8 +143,8 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
                     }
                     const int e0 = HALF ? e : 2 * e, e1 = HALF ? e + half : 2 * e + 1;
                     const float x = get1(it.x, e0), y = get1(it.x, e1);
-                    put1(it.y, e0, a.amplitude * (x * c[e].x - y * c[e].y));
-                    put1(it.y, e1, a.amplitude * (x * c[e].y + y * c[e].x));
+                    put1(it.y, e0, x * c[e].x - y * c[e].y);
+                    put1(it.y, e1, x * c[e].y + y * c[e].x);
                 }
                 continue;
             }
@@ -146,15 +154,15 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
 #pragma unroll
                     for (int e = 0; e < V; e += 2) {
                         const float x0 = get(p0[u], e), y0 = get(p1[u], e), x1 = get(p0[u], e + 1), y1 = get(p1[u], e + 1);
-                        put(o0, e, a.amplitude * (x0 * c[e].x - y0 * c[e].y), a.amplitude * (x1 * c[e + 1].x - y1 * c[e + 1].y));
-                        put(o1, e, a.amplitude * (x0 * c[e].y + y0 * c[e].x), a.amplitude * (x1 * c[e + 1].y + y1 * c[e + 1].x));
+                        put(o0, e, x0 * c[e].x - y0 * c[e].y, x1 * c[e + 1].x - y1 * c[e + 1].y);
+                        put(o1, e, x0 * c[e].y + y0 * c[e].x, x1 * c[e + 1].y + y1 * c[e + 1].x);
                     }
                     store(it.y + second, it.skip, o1);
                 } else {
 #pragma unroll
                     for (int e = 0; e < V; e += 2) {
                         const float x = get(p0[u], e), y = get(p0[u], e + 1), cc = c[e / 2].x, s = c[e / 2].y;
-                        put(o0, e, a.amplitude * (x * cc - y * s), a.amplitude * (x * s + y * cc));
+                        put(o0, e, x * cc - y * s, x * s + y * cc);
                     }
                 }
             }
@@ -170,7 +178,8 @@ __global__ void __launch_bounds__(RO_THREADS) rotary_kernel(RotaryArgs a, int to
 
 hipError_t launch_rotary(const RotaryArgs& a, int act_dtype, hipStream_t stream) {
     const int V = act_dtype == 1 ? 8 : 4, pairs = a.interleaved ? V / 2 : V;
-    const int64_t per_token = (a.n_heads + a.n_kv_heads) * (ceil_div(a.rot_dim / 2, pairs) + ceil_div(a.head_dim - a.rot_dim, V));
+    const int64_t per_head = ceil_div(a.rot_dim / 2, pairs) + ceil_div(a.head_dim - a.rot_dim, V);
+    const int64_t per_token = (a.n_heads + a.n_kv_heads) * per_head;  // at most 65535 heads of 129 pieces: the divisors are exact
     // about 512 items a workgroup (two a thread), but no fewer than 1024 workgroups for it
     int64_t tokens = ceil_div(512, per_token);
     if (tokens > a.T / 1024) tokens = a.T / 1024;
@@ -179,7 +188,8 @@ hipError_t launch_rotary(const RotaryArgs& a, int act_dtype, hipStream_t stream)
     const auto kernel = act_dtype == 1 ? (a.interleaved ? rotary_kernel<true, false> : rotary_kernel<true, true>)
                                        : (a.interleaved ? rotary_kernel<false, false> : rotary_kernel<false, true>);
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(ceil_div(a.T, tokens))), dim3(RO_THREADS),
-                       tokens * (a.rot_dim / 2) * sizeof(float2), stream, a, static_cast<int>(tokens));
+                       tokens * (a.rot_dim / 2) * sizeof(float2), stream, a, static_cast<int>(tokens),
+                       Divisor(per_token), Divisor(per_head));
     return hipGetLastError();
 }
 

@@ -50,6 +50,7 @@ def test_rotary_apply():
     assert _apply(T=0, q=None, k=None, qo=None, ko=None, freqs=None) == OK
     assert _apply(T=-1) == SHAPE and _apply(T=1 << 24) == SHAPE and _apply(T=1 << 31) == SHAPE
     assert _apply(H=0) == SHAPE and _apply(Hkv=-1) == SHAPE and _apply(H=70000) == SHAPE
+    assert _apply(H=40000, Hkv=40000, qs=1 << 30, qos=1 << 30, ks=1 << 30, kos=1 << 30) == SHAPE
     assert _apply(qs=127) == SHAPE and _apply(qos=127) == SHAPE and _apply(ks=63) == SHAPE and _apply(kos=0) == SHAPE
     assert _apply(rot=_rot(rot_dim=7)) == SHAPE
     assert _apply(dt=2) == ARG and _apply(backward=2) == ARG and _apply(amplitude=math.nan) == ARG
