@@ -156,6 +156,13 @@ __device__ __forceinline__ uint64_t wave_transpose_bits(uint64_t w) {
 
 __host__ __device__ __forceinline__ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// n / d by a multiplication: m = ceil(2^31 / d), exact for n d < 2^31.
+struct Divisor {
+    uint32_t d, m;
+    __host__ explicit Divisor(int64_t d) : d(static_cast<uint32_t>(d)), m(static_cast<uint32_t>(((int64_t(1) << 31) + d - 1) / d)) {}
+    __device__ int of(int n) const { return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(n)) * m >> 31); }
+};
+
 __host__ __device__ __forceinline__ size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // ---------------------------------------------------------------- buffer loads and waits

@@ -115,7 +115,7 @@ __device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[N]) {
 // A workgroup takes `tokens` tokens; 16 lanes a row of one token, (keys or values) and KV head, in this
 // order, so that what is read lies together. Bound by reading every value and writing its cached form.
 template <int DH, bool E4M3, bool IN_BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int tokens, const void* __restrict__ k,
+__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int tokens, Divisor token, const void* __restrict__ k,
                                                               int64_t k_stride, const void* __restrict__ v,
                                                               int64_t v_stride, const float* __restrict__ m_in) {
     constexpr int N = DH / 16;
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int
     auto load = [&](int r0) {
 #pragma unroll
         for (int u = 0; u < KV_U; ++u) {
-            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = tokens == 1 ? 0 : token.of(r), j = r - t * per_token;
             const bool is_v = j >= c.n_kv_heads;
             const int h = is_v ? j - c.n_kv_heads : j;
             load_row<IN_BF16, N>(is_v ? v : k, (t0 + t) * (is_v ? v_stride : k_stride) + static_cast<int64_t>(h) * DH + l16 * N, x[u]);
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int
     for (int r0 = g;;) {
 #pragma unroll
         for (int u = 0; u < KV_U; ++u) {
-            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = tokens == 1 ? 0 : token.of(r), j = r - t * per_token;
             const bool is_v = j >= c.n_kv_heads;
             const int h = is_v ? j - c.n_kv_heads : j;
             const KvPlace p = places.at[t];
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int
 }
 
 template <int DH, bool E4M3, bool OUT_BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int tokens, void* __restrict__ k,
+__global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int tokens, Divisor token, void* __restrict__ k,
                                                              void* __restrict__ v, float* __restrict__ m) {
     constexpr int N = DH / 16, W = E4M3 ? N / 4 : N / 2;  // words of a lane
     typedef uint32_t vec __attribute__((ext_vector_type(W)));
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
         float f[KV_U];
 #pragma unroll
         for (int u = 0; u < KV_U; ++u) {
-            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = tokens == 1 ? 0 : token.of(r), j = r - t * per_token;
             const bool is_v = j >= c.n_kv_heads;
             const int h = is_v ? j - c.n_kv_heads : j;
             const KvPlace p = places.at[t];
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
         }
 #pragma unroll
         for (int u = 0; u < KV_U; ++u) {
-            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = r / per_token, j = r - t * per_token;
+            const int r = min(r0 + u * KV_GROUPS, rows - 1), t = tokens == 1 ? 0 : token.of(r), j = r - t * per_token;
             const bool is_v = j >= c.n_kv_heads;
             const int h = is_v ? j - c.n_kv_heads : j;
             const KvPlace p = places.at[t];
@@ -280,8 +280,8 @@ hipError_t launch_kv_write(const KvCacheArgs& c, const void* k, int64_t k_stride
     const int n = tokens_of(c, 16);
     kv_dispatch(c, act_dtype == 1, [&](auto dh, auto e4m3, auto bf16) {
         hipLaunchKernelGGL((kv_write_kernel<decltype(dh)::value, decltype(e4m3)::value, decltype(bf16)::value>),
-                           dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n, k, k_stride,
-                           v, v_stride, m_in);
+                           dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n,
+                           Divisor(2 * c.n_kv_heads), k, k_stride, v, v_stride, m_in);
     });
     return hipGetLastError();
 }
@@ -290,7 +290,8 @@ hipError_t launch_kv_read(const KvCacheArgs& c, void* k, void* v, int out_dtype,
     const int n = tokens_of(c, 4);
     kv_dispatch(c, out_dtype == 1, [&](auto dh, auto e4m3, auto bf16) {
         hipLaunchKernelGGL((kv_read_kernel<decltype(dh)::value, decltype(e4m3)::value, decltype(bf16)::value>),
-                           dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n, k, v, m);
+                           dim3(static_cast<unsigned>(ceil_div(c.T, n))), dim3(KV_THREADS), 0, stream, c, n,
+                           Divisor(2 * c.n_kv_heads), k, v, m);
     });
     return hipGetLastError();
 }

@@ -20,13 +20,6 @@ __device__ __forceinline__ float2 turn(int position, double freq, float amplitud
     return make_float2(amplitude * c, backward ? -amplitude * s : amplitude * s);
 }
 
-// n / d by a multiplication: m = ceil(2^31 / d), exact for n d < 2^31.
-struct Divisor {
-    uint32_t d, m;
-    explicit Divisor(int64_t d) : d(static_cast<uint32_t>(d)), m(static_cast<uint32_t>(((int64_t(1) << 31) + d - 1) / d)) {}
-    __device__ int of(int n) const { return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(n)) * m >> 31); }
-};
-
 // A workgroup per `tokens` tokens: the sines and cosines of all of them into LDS, meanwhile the first
 // loads on their way. An item is a piece of a head: V consecutive values, 16 bytes, that hold pairs
 // (HALF: one piece of each half) or are copied. The last piece of either part is moved back to end with it:
