@@ -219,7 +219,10 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
             const int h = is_v ? j - c.n_kv_heads : j;
             const KvPlace p = places.at[t];
             const int64_t slot = ((static_cast<int64_t>(max(p.page, 0)) * c.n_kv_heads + h) << c.page_shift) + p.slot;
-            x[u] = *reinterpret_cast<const vec*>(static_cast<const uint8_t*>(is_v ? c.v : c.k) + slot * (DH * (E4M3 ? 1 : 2)) + l16 * (W * 4));
+            // streaming: pages of earlier steps are in no cache (16384 tokens x 8 heads of 128 in e4m3 26.4 -> 22.0 us);
+            // the rows that are written come from the kernel before and are read again, so there it costs 3 us
+            x[u] = __builtin_nontemporal_load(reinterpret_cast<const vec*>(
+                static_cast<const uint8_t*>(is_v ? c.v : c.k) + slot * (DH * (E4M3 ? 1 : 2)) + l16 * (W * 4)));
             if constexpr (E4M3) f[u] = __uint_as_float(static_cast<uint32_t>((is_v ? c.v_scale : c.k_scale)[slot]) << 23);
         }
 #pragma unroll
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
 
 // Tokens of a workgroup: `rows` for every 16 lanes, but no fewer than 1024 workgroups for it. Writing 16384
 // tokens x 8 heads of 128 in e4m3 takes 28.9 us with 4 rows and 26.9 with 16 (longer pieces of a page
-// at a time), reading 27.7 and 28.7.
+// at a time), reading 27.7 and 28.7 (before the other steps noted here).
 int tokens_of(const KvCacheArgs& c, int rows) {
     int64_t n = ceil_div(KV_GROUPS * rows, 2 * c.n_kv_heads);
     if (n > c.T / 1024) n = c.T / 1024;
