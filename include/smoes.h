@@ -803,7 +803,9 @@ size_t smoes_attention_decode_workspace_size(const smoes_kv_cache* cache, int n_
  * o          [n_seq, n_heads, head_dim] bf16 output.
  * m_heads    [n_seq, n_heads, 2] float32 output, as smoes_attn_score_update takes it;
  *            required iff cache->m is not NULL.
- * The cached rows enter as they are read back; products and sums are float32.
+ * The cached rows enter as they are read back; products and sums are float32, the sums
+ * over weights of up to 2^8 that are divided by their sum at the end: they are finite
+ * for values below 2^119 / seq_lens[b].
  * The split of the work follows from all sequences' lengths: the same call gives
  * the same bits. n_heads % n_kv_heads == 0, n_seq * n_heads < 2^24. Asynchronous on `stream`;
  * nothing is allocated; the workspace needs no initialisation.

@@ -96,7 +96,6 @@ struct Share {
     }
 };
 
-
 __device__ __forceinline__ int seq_len(int len, int cap) { return min(max(len, 0), cap); }
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -612,7 +611,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             if (lane < QR)  // vision, text, sum (-1: no key seen), maximum
                 *reinterpret_cast<f32x4_t*>(dst + DH) = f32x4_t{acc[rt][T::VN][0], acc[rt][T::VN][1], seen ? acc[rt][T::VN][2] : -1.f, m_run[rt]};
             __syncthreads();
-                float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH) + rt * QR * PITCH;
+            float* out = part + (static_cast<int64_t>(2 * w + (first ? 0 : 1))) * partial_floats(a.rows, DH) + rt * QR * PITCH;
             for (int x = threadIdx.x; x < rows * (DH / 4); x += DE_THREADS) {
                 const int r = x / (DH / 4), d = x % (DH / 4) * 4;
                 f32x4_t y[DE_WAVES];

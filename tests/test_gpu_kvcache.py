@@ -109,6 +109,28 @@ def test_one_token_each(kind, n_seq):
     read_check(c, cache, table, lens, None, n_seq, "bf16")
 
 
+@pytest.mark.parametrize("kind,dtype", [("bf16", "bf16"), ("e4m3", "f32")])
+@pytest.mark.parametrize("n_seq,longest,Hkv,dh", [(1022, 4, 5, 64), (1023, 3, 1, 128), (1024, 9, 3, 64), (1500, 45, 1, 64),
+                                                  (37, 130, 8, 128), (3, 1500, 2, 64)])
+def test_many_tokens_and_sequences(kind, dtype, n_seq, longest, Hkv, dh):
+    # several tokens of different sequences per workgroup (up to 32), offsets that fit its memory and ones that do not
+    say("kv many", kind, dtype, n_seq, longest)
+    rng = np.random.default_rng(n_seq)
+    new = rng.integers(0, longest, n_seq)
+    new[n_seq // 2] = 0
+    new[n_seq // 3] = longest
+    lens = (new + rng.integers(0, 20, n_seq)).astype(np.int32)
+    c, cache, table = make(rng, lens, 16, Hkv, dh, kind)
+    off = np.concatenate([[0], new.cumsum()]).astype(np.int32)
+    T = int(off[-1]) + 3
+    k, v = rows(rng, T, Hkv, dh, dtype), rows(rng, T, Hkv, dh, dtype)
+    m = rng.uniform(0, 1, (T, 2)).astype(np.float32)
+    S.kv_write(cache, t(table), t(lens), t(k), t(v), t(m), sample_offsets=t(off))
+    V.kv_write(c, table, lens, off, k, v, m)
+    same(c, cache)
+    read_check(c, cache, table, lens, off, T, dtype)
+
+
 def test_places_that_are_not_held():
     # unheld pages (-1 and past the pool), lengths past the table, negative lengths, fewer held than new tokens
     say("kv places")

@@ -57,6 +57,10 @@ CASES = [  # T, H, Hkv, head_dim, rot_dim, layout, scaling, dtype
     (11, 1, 1, 12, 12, "half", "none", torch.bfloat16),
     (3, 2, 2, 7, 6, "half", "none", torch.float32),
     (3, 2, 2, 31, 30, "interleaved", "none", torch.bfloat16),
+    (2051, 3, 2, 64, 64, "half", "none", torch.bfloat16),        # two and more tokens of a workgroup, the last one short
+    (5003, 2, 1, 128, 96, "interleaved", "ntk", torch.bfloat16),
+    (17001, 1, 1, 64, 22, "half", "none", torch.float32),
+    (16411, 1, 0, 8, 6, "interleaved", "linear", torch.bfloat16),
 ]
 
 
