@@ -347,6 +347,49 @@ def test_generation_matches_the_whole_sample(kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_captured_step_replayed(kind):
+    # one step (rotary, cache, decode, read back) captured with its lengths; every replay, with new rows and eager
+    # work between, gives the bits of the eager step on a second cache, across ends of pages and of tiles
+    say("captured step", kind)
+    rng = np.random.default_rng(21)
+    H, Hkv, dh, page, steps = 8, 2, 128, 16, 6
+    start = np.array([125, 0, 14, 300], np.int32)
+    c, cache, table = make(rng, start + steps, page, Hkv, dh, kind)
+    twin = to_device(c)
+    tb, n = t(table), len(start)
+    plan = S.RotaryPlan(S.RotarySpec(dh, dh), DEV)
+
+    def step(cache, ln, qkv, m_in, ws):
+        ln += 1
+        q, k = S.rotary(plan, qkv[:, :H], qkv[:, H:H + Hkv], positions=ln - 1)
+        S.kv_write(cache, tb, ln, k, qkv[:, H + Hkv:], m_in)
+        return S.attention_scores_decode(cache, tb, ln, q, workspace=ws) + S.kv_read(cache, tb, ln)
+
+    ws, ws2 = (torch.empty(S.attention_decode_workspace_bytes(cache, n, H), dtype=torch.uint8, device=DEV) for _ in range(2))
+    qkv = torch.zeros((n, H + 2 * Hkv, dh), dtype=torch.bfloat16, device=DEV)
+    m_in = torch.zeros((n, 2), device=DEV)
+    ln, ln2 = t(start.copy()), t(start.copy())
+    step(to_device(c), t(start.copy()), qkv, m_in, ws)  # loads the kernels
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        got = step(cache, ln, qkv, m_in, ws)
+    for s in range(steps):
+        qkv.copy_(torch.from_numpy(rng.standard_normal(tuple(qkv.shape)).astype(np.float32)))
+        m_in.copy_(torch.from_numpy(rng.uniform(0, 1, (n, 2)).astype(np.float32)))
+        graph.replay()
+        want = step(twin, ln2, qkv, m_in, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(ln, ln2) and ln.tolist() == (start + s + 1).tolist()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+    for x, y in zip((cache.k, cache.v, cache.k_scale, cache.m), (twin.k, twin.v, twin.k_scale, twin.m)):
+        assert x is None and y is None or torch.equal(x, y)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("dh,H,Hkv", [(64, 4, 2), (128, 16, 2), (64, 18, 1)])
 def test_more_tiles_than_workgroups(kind, dh, H, Hkv):
     # every workgroup has several tiles, most of more than one (sequence, group)
