@@ -407,10 +407,11 @@ def _gpu_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
 # the handle of a GPU's current stream, without the Stream object where torch offers that
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _launch(dev: int, where: str, fn, *args) -> None:
-    if dev == torch.cuda.current_device():
+    if dev == _current_gpu():
         status = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
@@ -435,6 +436,10 @@ def _heads(t: torch.Tensor, name: str, dtype, n: int, h: int, d: int) -> int:
     if (s2 == 1 or d == 1) and (s1 == d or h == 1) and (s0 >= h * d or n == 1):
         return s0 if n > 1 else h * d
     raise ValueError(f"{name}: the heads of a token have to be dense (strides {t.stride()})")
+
+
+def _dense_like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _array(t: Optional[torch.Tensor], name: str, dtype, shape) -> None:
@@ -507,14 +512,14 @@ def rotary(plan: RotaryPlan, q: torch.Tensor, k: Optional[torch.Tensor] = None,
     T, H = _sizes(q, "q", dh)
     q_stride = _heads(q, "q", dtype, T, H, dh)
     if q_out is None:
-        q_out = torch.empty((T, H, dh), dtype=dtype, device=q.device)
+        q_out = _dense_like(q)
     qo_stride = _heads(q_out, "q_out", dtype, T, H, dh)
     Hkv = k_stride = ko_stride = 0
     if k is not None:
         Hkv = _sizes(k, "k", dh)[1]
         k_stride = _heads(k, "k", dtype, T, Hkv, dh)
         if k_out is None:
-            k_out = torch.empty((T, Hkv, dh), dtype=dtype, device=q.device)
+            k_out = _dense_like(k)
         ko_stride = _heads(k_out, "k_out", dtype, T, Hkv, dh)
     elif k_out is not None:
         raise ValueError("k_out without k")
@@ -568,13 +573,14 @@ class KVCache:
 
 def _kv_tables(block_table: torch.Tensor, seq_lens: torch.Tensor, sample_offsets: Optional[torch.Tensor]):
     """Sequences and pages of a row of the block table."""
-    if seq_lens.dim() != 1 or block_table.dim() != 2:
+    shape = block_table.shape
+    if len(shape) != 2 or seq_lens.shape != shape[:1]:
         raise ValueError("seq_lens is [n_seq], block_table [n_seq, max_pages]")
-    n_seq, max_pages = seq_lens.shape[0], block_table.shape[1]
-    _array(seq_lens, "seq_lens", torch.int32, (n_seq,))
-    _array(block_table, "block_table", torch.int32, (n_seq, max_pages))
-    _array(sample_offsets, "sample_offsets", torch.int32, (n_seq + 1,))
-    return n_seq, max_pages
+    _array(seq_lens, "seq_lens", torch.int32, shape[:1])
+    _array(block_table, "block_table", torch.int32, shape)
+    if sample_offsets is not None:
+        _array(sample_offsets, "sample_offsets", torch.int32, (shape[0] + 1,))
+    return shape
 
 
 def kv_write(cache: KVCache, block_table: torch.Tensor, seq_lens: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -633,9 +639,9 @@ def attention_scores_decode(cache: KVCache, block_table: torch.Tensor, seq_lens:
     shape = (n_seq, H, cache.head_dim)
     q_stride = _heads(q, "q", torch.bfloat16, *shape)
     if o is None:
-        o = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        o = _dense_like(q)
     if m_heads is None and cache.m is not None:
-        m_heads = torch.empty((n_seq, H, 2), dtype=torch.float32, device=q.device)
+        m_heads = q.new_empty((n_seq, H, 2), dtype=torch.float32)
     _array(o, "o", torch.bfloat16, shape)
     _array(m_heads, "m_heads", torch.float32, (n_seq, H, 2))
     if workspace is None:
