@@ -161,17 +161,20 @@ __device__ __forceinline__ float max_over_groups(float x) {
 }
 
 // Two probabilities as bf16 pairs whose sum is x to 2^-23: hi and mid are cut below the value (of x (1 - 2^-8),
-// of the rest likewise), so that no term of a positive x is zero or negative and an infinite value stays infinite.
+// of the rest likewise), so that no term of a positive x is zero or negative and an infinite value stays infinite; a
+// term that would fall under the smallest bf16 value, 2^-133, is that value.
 struct Split {
     uint32_t hi, mid, lo;
 };
 __device__ __forceinline__ Split split_pair(float x0, float x1) {
     constexpr float c = 1.f - 0x1p-8f;
     Split s;
+    const uint32_t least0 = min(__float_as_uint(x0), 0x10001u), least1 = min(__float_as_uint(x1), 0x10001u);
+    auto at_least = [](float x, uint32_t least) { return __uint_as_float(max(__float_as_uint(x), least)); };
     auto cut = [&](float& a, float& b) {  // the upper halves of a c and b c; a and b become what is left
-        const uint32_t u = __float_as_uint(a * c), v = __float_as_uint(b * c);
-        a -= __uint_as_float(u & 0xffff0000u);
-        b -= __uint_as_float(v & 0xffff0000u);
+        const uint32_t u = max(__float_as_uint(a * c), least0), v = max(__float_as_uint(b * c), least1);
+        a = at_least(a - __uint_as_float(u & 0xffff0000u), least0);
+        b = at_least(b - __uint_as_float(v & 0xffff0000u), least1);
         return __builtin_amdgcn_perm(v, u, 0x07060302u);
     };
     s.hi = cut(x0, x1);
