@@ -23,7 +23,7 @@
 //   v_mfma_f32_4x4x1f32, which treats four lanes by themselves, multiplies a key's four column pieces by its
 //   four probabilities in float32: 8 cycles for a column of 16 lanes, a quarter of the 16 x 16 form's.
 //   Larger groups (QR = 16): v_mfma_f32_16x16x32_bf16 over the tile's 32 keys per column, the probabilities as
-//   three bf16 terms whose sum is the float32 value to 2^-23: 48 cycles per column for the 256 of the float32 form (64
+//   three bf16 terms whose sum is the float32 value, bit for bit: 48 cycles per column for the 256 of the float32 form (64
 //   heads over 8 in e4m3, 64 sequences of 200 to 20000: 146 -> 120 us; 40 over 2 in bf16: 44 -> 36).
 // The scores are carried by one more 4 x 4 product per key, float32: vision, text and 1 (the softmax
 // denominator).
@@ -160,25 +160,26 @@ __device__ __forceinline__ float max_over_groups(float x) {
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Two probabilities as bf16 pairs whose sum is x to 2^-23: hi and mid are cut below the value (of x (1 - 2^-8),
-// of the rest likewise), so that no term of a positive x is zero or negative and an infinite value stays infinite; a
-// term that would fall under the smallest bf16 value, 2^-133, is that value.
+// Two probabilities as bf16 pairs hi + mid + lo that sum to x in all 24 bits. hi and mid are the largest bf16
+// value below what is left (bits - 1, the upper half): at most 2^16 steps of x's last bit are left by hi, and by mid
+// a number of eight bits, which lo holds as it is. What is left is never zero, so that an infinite value times a
+// positive x is infinite in every term; a term that would fall under the smallest bf16 value, 2^-133, is that value (of an
+// x below 2^-109 the sum is off by up to 2^-132). The terms of zero are zeros.
 struct Split {
     uint32_t hi, mid, lo;
 };
 __device__ __forceinline__ Split split_pair(float x0, float x1) {
-    constexpr float c = 1.f - 0x1p-8f;
     Split s;
     const uint32_t least0 = min(__float_as_uint(x0), 0x10001u), least1 = min(__float_as_uint(x1), 0x10001u);
-    auto at_least = [](float x, uint32_t least) { return __uint_as_float(max(__float_as_uint(x), least)); };
-    auto cut = [&](float& a, float& b) {  // the upper halves of a c and b c; a and b become what is left
-        const uint32_t u = max(__float_as_uint(a * c), least0), v = max(__float_as_uint(b * c), least1);
-        a = at_least(a - __uint_as_float(u & 0xffff0000u), least0);
-        b = at_least(b - __uint_as_float(v & 0xffff0000u), least1);
+    auto cut = [&]() {
+        const uint32_t u = __builtin_elementwise_sub_sat(__float_as_uint(x0), 1u) & 0xffff0000u;
+        const uint32_t v = __builtin_elementwise_sub_sat(__float_as_uint(x1), 1u) & 0xffff0000u;
+        x0 = __uint_as_float(max(__float_as_uint(x0 - __uint_as_float(u)), least0));
+        x1 = __uint_as_float(max(__float_as_uint(x1 - __uint_as_float(v)), least1));
         return __builtin_amdgcn_perm(v, u, 0x07060302u);
     };
-    s.hi = cut(x0, x1);
-    s.mid = cut(x0, x1);
+    s.hi = cut();
+    s.mid = cut();
     s.lo = cvt_bf16x2(x0, x1);
     return s;
 }
