@@ -777,7 +777,7 @@ int smoes_kv_write(const smoes_kv_cache* cache, const int32_t* block_table, int6
  * Read rows back: the same places as smoes_kv_write's, that is the last n_b
  * tokens of every sequence (all of them with n_b = seq_lens[b]), dense, for
  * smoes_attention_scores over a context that is in the cache.
- * k, v       [T, n_kv_heads, head_dim] outputs of act_dtype, or NULL (not wanted).
+ * k, v       [T, n_kv_heads, head_dim] outputs of act_dtype, or NULL (not wanted), from any element on.
  * m          [T, 2] float32 output, or NULL.
  * A token that has no place reads as zeros; rows behind sample_offsets[n_seq] are
  * left as they were.
@@ -800,7 +800,7 @@ size_t smoes_attention_decode_workspace_size(const smoes_kv_cache* cache, int n_
  * page) gets zeros. What the pages hold at or behind the length does not enter, NaN or not.
  * q          [n_seq, n_heads, head_dim] bf16, q_stride elements from sequence to sequence. o must not overlap it.
  * scale      logit scale; <= 0 selects 1 / sqrt(head_dim).
- * o          [n_seq, n_heads, head_dim] bf16 output.
+ * o          [n_seq, n_heads, head_dim] bf16 output, from any element on.
  * m_heads    [n_seq, n_heads, 2] float32 output, as smoes_attn_score_update takes it;
  *            required iff cache->m is not NULL.
  * The cached rows enter as they are read back; products and sums are float32, the sums

@@ -69,10 +69,10 @@ struct DecodeArgs {
     float* m_heads;
 };
 
-// Four dims of a head's output, and with the first four its scores.
+// Four dims of a head's output (at any element), and with the first four its scores.
 __device__ __forceinline__ void store_row4(const DecodeArgs& a, int64_t head, int dh, int d, f32x4_t o, f32x4_t m) {
-    *reinterpret_cast<uint2*>(a.o + head * dh + d) =
-        make_uint2(cvt_bf16x2(o[0], o[1]), cvt_bf16x2(o[2], o[3]));
+    typedef uint32_t row4 __attribute__((ext_vector_type(2), aligned(2)));
+    *reinterpret_cast<row4*>(a.o + head * dh + d) = row4{cvt_bf16x2(o[0], o[1]), cvt_bf16x2(o[2], o[3])};
     if (d == 0 && a.m_heads != nullptr) {
         a.m_heads[2 * head] = m[0];
         a.m_heads[2 * head + 1] = m[1];

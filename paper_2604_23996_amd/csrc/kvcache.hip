@@ -103,9 +103,10 @@ __device__ __forceinline__ void load_row(const void* base, int64_t i, float (&x)
         }
     }
 }
-template <int N>
+// N words at a multiple of A bytes: all of them in the cache, an element's in the outputs.
+template <int A, int N>
 __device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[N]) {
-    typedef uint32_t vec __attribute__((ext_vector_type(N)));
+    typedef uint32_t vec __attribute__((ext_vector_type(N), aligned(A)));
     vec r;
 #pragma unroll
     for (int i = 0; i < N; ++i) r[i] = w[i];
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int
                     }
                 }
                 if (keep) {
-                    store_words(static_cast<uint8_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
+                    store_words<N>(static_cast<uint8_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
                     if (l16 == 0) (is_v ? c.v_scale : c.k_scale)[slot] = static_cast<uint8_t>(ex + 127);
                 }
             } else {
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvCacheArgs c, int
 #pragma unroll
                 for (int e = 0; e < N; e += 2)
                     w[e / 2] = cvt_bf16x2(x[u][e], x[u][e + 1]);
-                if (keep) store_words(static_cast<uint16_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
+                if (keep) store_words<2 * N>(static_cast<uint16_t*>(is_v ? c.v : c.k) + slot * DH + l16 * N, w);
             }
         }
         r0 += KV_U * KV_GROUPS;
@@ -249,12 +250,12 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
                 uint32_t w[N / 2];
 #pragma unroll
                 for (int i = 0; i < N; i += 2) w[i / 2] = cvt_bf16x2(e[i], e[i + 1]);
-                store_words(static_cast<uint16_t*>(y) + at, w);
+                store_words<2>(static_cast<uint16_t*>(y) + at, w);
             } else {
 #pragma unroll
                 for (int i = 0; i < N; i += 4) {
                     const uint32_t w[4] = {__float_as_uint(e[i]), __float_as_uint(e[i + 1]), __float_as_uint(e[i + 2]), __float_as_uint(e[i + 3])};
-                    store_words(static_cast<float*>(y) + at + i, w);
+                    store_words<4>(static_cast<float*>(y) + at + i, w);
                 }
             }
         }
