@@ -487,6 +487,7 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             }
             // ---- probabilities, values, scores
             Split ps[QR == 16 ? RT : 1][NS][2];  // of keys 0 and 1, 2 and 3 of a piece
+            float v_scale[NS][4];
 #pragma unroll
             for (int p = 0; p < NS; ++p) {
                 const int nv = t.nv[p];
@@ -498,11 +499,12 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
                     const int m_own = t.m[e], m_next = QR == 16 ? dpp_mov<0x124>(m_own) : m_own;
                     const int m = (l16 >> 2 & 1) == p ? m_own : m_next;
                     const float mc = __int_as_float((m & (in ? score_mask[p] : 0)) | one[p]);
+                    if constexpr (E4M3 && QR == 16) v_scale[p][e] = in ? scale_of(vs[p], e) : 1.f;
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
                         const float pr = __builtin_amdgcn_exp2f(s[rt][p][e] - from[rt]);
                         pv[rt][e] = pr;
-                        if constexpr (E4M3) pv[rt][e] = in ? pr * scale_of(vs[p], e) : 0.f;
+                        if constexpr (E4M3 && QR == 4) pv[rt][e] = in ? pr * scale_of(vs[p], e) : 0.f;
                         acc[rt][T::VN] = __builtin_amdgcn_mfma_f32_4x4x1f32(mc, pr, acc[rt][T::VN], 0, 0, 0);
                     }
                     if constexpr (QR == 4) {
@@ -542,10 +544,16 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             if constexpr (E4M3) {
-                                const uint32_t x = __builtin_amdgcn_perm(t.v[p][2 * i + 1][n / 4], t.v[p][2 * i][n / 4],
-                                                                         n & 2 ? 0x07030602u : 0x05010400u);
-                                v0.w[2 * p + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
-                                v1.w[2 * p + i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true));
+                                // the values as they are read back, code times scale: bf16 values. (The scale in the
+                                // probability would push its lower terms under the smallest bf16 value.)
+                                auto two = [&](int e) {
+                                    const int x = t.v[p][e][n / 4];
+                                    return __builtin_bit_cast(uint32_t, n & 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, v_scale[p][e], true)
+                                                                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, v_scale[p][e], false));
+                                };
+                                const uint32_t x0 = two(2 * i), x1 = two(2 * i + 1);
+                                v0.w[2 * p + i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+                                v1.w[2 * p + i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
                             } else {
                                 v0.w[2 * p + i] = __builtin_amdgcn_perm(t.v[p][2 * i + 1][n / 2], t.v[p][2 * i][n / 2], 0x05040100u);
                                 v1.w[2 * p + i] = __builtin_amdgcn_perm(t.v[p][2 * i + 1][n / 2], t.v[p][2 * i][n / 2], 0x07060302u);
