@@ -382,8 +382,12 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
         score_mask[p] = mine && (lane & 3) < 2 ? -1 : 0;
         one[p] = mine && (lane & 3) == 2 ? 0x3f800000 : 0;
     }
-    auto scales_of = [&](int which, int p) {  // which: 0 keys, 1 values
-        return __builtin_amdgcn_ds_bpermute(4 * ((lane & 48) + 8 * which + 4 * p + g4), t.scales);
+    auto value_scales = [&](int p) {  // four bytes, of the values that meet this lane's probabilities
+        return __builtin_amdgcn_ds_bpermute(4 * ((lane & 48) + 8 + 4 * p + g4), t.scales);
+    };
+    auto key_scale = [&](int p) {  // of key l % 16
+        const int four = __builtin_amdgcn_ds_bpermute(4 * ((lane & 48) + 4 * p + (l16 >> 2)), t.scales);
+        return __uint_as_float((static_cast<uint32_t>(four) >> (8 * (l16 & 3)) & 0xffu) << 23);
     };
 
     fetch();
@@ -424,22 +428,22 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
             for (int p = 0; p < NS; ++p) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) s[rt][p] = f32x4_t{};
-                int ks = 0;
+                float ks = 1.f;  // of this lane's key
                 if constexpr (E4M3) {
-                    ks = scales_of(0, p);
-                    vs[p] = scales_of(1, p);
+                    ks = key_scale(p);
+                    vs[p] = value_scales(p);
                 }
 #pragma unroll
                 for (int c = 0; c < NQ; ++c) {
                     bf16x8_t kf;
                     if constexpr (E4M3) {
-                        // e4m3 values are bf16 values; the row's scale goes to the logit
+                        // the row as it is read back, code times scale: bf16 values
                         union { bf16x8_t v; bf16x2_t h[4]; } u;
                         const int x0 = t.k[p][c >> 1][2 * (c & 1)], x1 = t.k[p][c >> 1][2 * (c & 1) + 1];
-                        u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, 1.f, false);
-                        u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, 1.f, true);
-                        u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, 1.f, false);
-                        u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, 1.f, true);
+                        u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, ks, false);
+                        u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, ks, true);
+                        u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, ks, false);
+                        u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, ks, true);
                         kf = u.v;
                     } else {
                         kf = __builtin_bit_cast(bf16x8_t, t.k[p][c]);
@@ -454,7 +458,6 @@ decode_kernel(DecodeArgs a, const uint16_t* __restrict__ q, const int32_t* __res
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
                         float x = s[rt][p][e] * a.scale_log2;
-                        if constexpr (E4M3) x *= scale_of(ks, e);
                         x = g4 * 4 + e < nk ? x : -INFINITY;
                         s[rt][p][e] = x;
                         mx[rt] = fmaxf(mx[rt], x);

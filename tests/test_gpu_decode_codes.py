@@ -63,6 +63,33 @@ def test_scales_far_from_one(H, dh):
     assert np.all(np.abs(host(mh) - ref_m) <= rel[..., None])
 
 
+@pytest.mark.parametrize("H,dh", [(8, 64), (8, 128), (32, 128), (40, 64)])
+def test_large_queries_on_small_keys(H, dh):
+    # queries of 2^117 to 2^119 on keys of 2^-119 or so: the products of what is read back are moderate, those of the codes
+    # with the queries are beyond float32
+    say("decode large queries", H, dh)
+    rng = np.random.default_rng(H + 2)
+    lens = np.array([300, 70], np.int32)
+    c, _, table = make(rng, lens, 16, 2, dh, "e4m3")
+    c["k"] = (c["k"] & 0x87) | rng.integers(8, 15, c["k"].shape).astype(np.uint8) << 3  # 2 to 256: no code near zero
+    c["k_scale"][:] = 10
+    q = V.bf16_round(queries_of(rng, 2, H, dh))
+    poison(c, table, lens)
+    o, mh = run(c, table, lens, q)
+    ref_o, ref_m, size, av, keys = V.attention_decode(c, table, lens, q)
+    rel = 2 * ((dh + 5) * U * size + 4 * U + (keys[:, None] + 64) * U)
+    # The logits lie thousands apart: weights below 2^-126 of the largest are zero in float32, up to 300 of them on values
+    # below 64 (codes of 448 at most, scales of 2^-3), 2^-111 together, all that is left of a column whose largest value is 0.
+    tol = rel[..., None] * av + 300 * 2.0 ** -126 * 64
+    tol = tol + 2.0 ** -8 * (np.abs(ref_o) + tol)
+    assert np.all(np.abs(host(o) - ref_o) <= tol)
+    assert np.all(np.abs(host(mh) - ref_m) <= rel[..., None])
+
+
+def queries_of(rng, n, H, dh):
+    return np.where(rng.random((n, H, dh)) < 0.5, -1.0, 1.0) * 2.0 ** rng.integers(117, 120, (n, H, dh))
+
+
 @pytest.mark.parametrize("H", [4, 16, 32])
 @pytest.mark.parametrize("e", [-112, -116])
 def test_weights_of_small_values_keep_their_bits(H, e):
