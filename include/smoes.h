@@ -24,7 +24,8 @@
  *
  * Conventions shared by every entry point
  *   - Every array pointer is a DEVICE pointer owned by the caller; arrays are
- *     dense and row-major (a token stride argument says where rows may lie apart). The library allocates no device memory: scratch
+ *     dense and row-major (a token stride argument says where rows may lie
+ *     apart). The library allocates no device memory: scratch
  *     comes from a caller-provided workspace whose size the matching
  *     *_workspace_size query returns (any alignment; the library aligns
  *     inside it). Workspace contents need not be initialised and are

@@ -6,6 +6,9 @@
 // query heads of a group share its rows. 128 sequences of 4169 tokens on average, 16 KV heads of 128 in
 // bf16 (4.4 GB), take 667 us, 6.6 TB/s; one of 131072, 32 heads over 8, 89 us (6.0); 64 of 200 to 20000 in
 // e4m3, 32 over 8, 108 us (5.1: 5 % more is fetched, lines of scales and scores, and the join takes 5 us of it).
+// With few tiles a workgroup no unit is the bound, but its start (lengths, block table, keys: loads that wait for each
+// other), its end and the join: 16 sequences of 2000 to 20000, 40 heads over 2, about four tiles each, take 36 us in
+// bf16 (3.6 TB/s) and 31 in e4m3 (2.1), 5.5 of it the join (address unit 40 and 22 % busy, vector ALUs 22 and 30, matrix cores 10).
 //
 // The work is cut evenly over a fixed number of workgroups, whatever the sequences' lengths are: the tiles
 // (128 keys of one sequence and group) of all sequences stand in one row, and the workgroups take the same
@@ -24,7 +27,9 @@
 //   four probabilities in float32: 8 cycles for a column of 16 lanes, a quarter of the 16 x 16 form's.
 //   Larger groups (QR = 16): v_mfma_f32_16x16x32_bf16 over the tile's 32 keys per column, the probabilities as
 //   three bf16 terms whose sum is the float32 value, bit for bit: 48 cycles per column for the 256 of the float32 form (64
-//   heads over 8 in e4m3, 64 sequences of 200 to 20000: 146 -> 120 us; 40 over 2 in bf16: 44 -> 36).
+//   heads over 8 in e4m3, 64 sequences of 200 to 20000: 146 -> 118 us; 40 over 2 in bf16: 44 -> 36).
+// The codes of an e4m3 row become bf16 values with the row's scale on their way into the bf16 products (exact); in
+// the float32 ones the scale of a value's row goes to its probability.
 // The scores are carried by one more 4 x 4 product per key, float32: vision, text and 1 (the softmax
 // denominator).
 #include "common.h"
