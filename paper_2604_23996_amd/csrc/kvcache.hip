@@ -222,8 +222,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvCacheArgs c, int 
             const int64_t slot = ((static_cast<int64_t>(max(p.page, 0)) * c.n_kv_heads + h) << c.page_shift) + p.slot;
             // streaming, for a context of earlier calls: in e4m3, 8 heads of 128, 65536 tokens take 64.0 us (with ordinary
             // loads 78.2), 16384 21.0 (21.6), 4096 8.2 (7.9). Rows that still are in the last-level cache lose by it, 16384
-            // read again and again 20.7 (18.0), but right behind their write, of which they spare the cache, write and
-            // read take 38.7 (41.2). The write's own loads, of rows that the kernel before has made, are ordinary ones.
+            // read again and again 20.7 (18.0); write and read behind each other take 38.7 (41.2), of 65536 172 (166).
+            // The write's own loads, of rows that the kernel before has made, are ordinary ones.
             x[u] = __builtin_nontemporal_load(reinterpret_cast<const vec*>(
                 static_cast<const uint8_t*>(is_v ? c.v : c.k) + slot * (DH * (E4M3 ? 1 : 2)) + l16 * (W * 4)));
             if constexpr (E4M3) f[u] = __uint_as_float(static_cast<uint32_t>((is_v ? c.v_scale : c.k_scale)[slot]) << 23);

@@ -115,3 +115,27 @@ def test_weights_of_small_values_keep_their_bits(H, e):
     o, mh = host(o)[:, :, 0], mh.cpu().double()[:, :, 0] * 2.0 ** e
     assert mh.min() >= 2.0 ** -126
     assert np.array_equal(o, host(mh.float().bfloat16())), np.mean(o != host(mh.float().bfloat16()))
+
+
+@pytest.mark.parametrize("H", [4, 16, 32])
+def test_one_key_returns_its_value_at_every_scale(H):
+    # every scale byte that a write leaves, 10 to 247, and every code (at 2^120 up to 1.875 * 2^127, the last value below
+    # infinity): a weight of 1 over a sum of 1, and the row as it is read back, a bf16 value, bit for bit
+    say("decode one key, all scales", H)
+    codes = np.concatenate([np.arange(127), np.arange(128, 255)]).astype(np.uint8)
+    codes = np.resize(codes, 4 * 64).reshape(4, 64)
+    scales = np.repeat(np.arange(10, 248), 4)
+    n = len(scales)
+    c, table, lens = two_keys("e4m3", n, 64)
+    lens[:] = 1
+    c["v"][:, 0, 0] = np.tile(codes, (n // 4, 1))
+    c["v"][scales == 247] &= 0xf7  # codes of at most 240: below 0x78
+    c["v_scale"][:, 0, 0] = scales
+    c["k_scale"][:, 0, 0] = scales[::-1]
+    c["m"][:, :, 0] = np.random.default_rng(H).uniform(0, 1, (n, 2))
+    q = V.bf16_round(np.random.default_rng(H + 1).standard_normal((n, H, 64)))
+    o, mh = run(c, table, lens, q)
+    want = V.E4M3[c["v"][:, 0, 0]] * 2.0 ** (scales - 127.0)[:, None]
+    assert np.abs(want).max() == 1.875 * 2.0 ** 127
+    assert np.array_equal(host(o), np.broadcast_to(want[:, None], o.shape))
+    assert np.array_equal(mh.cpu().numpy(), np.broadcast_to(c["m"][:, None, :, 0], mh.shape))
